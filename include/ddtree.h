@@ -250,6 +250,44 @@ int ddtree_compact(const void *k_tree, const void *v_tree, const int32_t *path,
                    int Hkv, int D, int elem_bytes, void *k_cache, void *v_cache, void *stream);
 
 /*
+ * A KV cache in 4 bits.  The head dim is cut into blocks of 32 elements; a block is one byte b, its power of two
+ * 2^(b - 127), and 32 codes of 4 bits: the sign (bit 3) and 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0-2), two codes a byte, the
+ * element of even index in the low half.  Head-major arrays of `cache_rows` rows, which sequences share as they do
+ * the rows of k_cache / v_cache:
+ *   k_codes, v_codes    [device] uint8 [Hkv, cache_rows, D/2], 16-byte aligned
+ *   k_scales, v_scales  [device] uint8 [Hkv, cache_rows, D/32], 4-byte aligned
+ * 4.25 bits an element.  As it is written a block gets the power of two for which its largest magnitude, rounded to two
+ * significant bits (ties to even), becomes 4 or 6 (from 2^-124 to 2^125), and every element the nearest code (ties to
+ * even): no element is off by more than half a step of the grid, that of the largest magnitude included (but magnitudes from
+ * 7 * 2^125 on become 6 * 2^125).  Values read back are exact in bf16.  A block that holds an infinity or a NaN gets the byte 255 and reads back as NaN.
+ * Common to the calls: D a multiple of 32 and at most 256, Hkv <= 32767, every row named below cache_rows
+ * (DDTREE_ERR_ARG otherwise); tensors of rows 16-byte aligned, dtype DDTREE_DTYPE_BF16 or DDTREE_DTYPE_FP32; rows
+ * that a call does not name keep their bytes.
+ *
+ * ddtree_q4_store writes prompts: rows src_offset[s] .. src_offset[s+1] - 1 of k / v become the rows from dst_row[s] on.
+ *   k, v        [device] [src_offset[batch], Hkv, D]
+ *   src_offset  [host] int32 [batch+1], non-decreasing, src_offset[0] >= 0
+ *   dst_row     [host] int32 [batch]; where destinations overlap, either sequence's row may stay
+ */
+int ddtree_q4_store(const void *k, const void *v, const int32_t *src_offset, const int32_t *dst_row,
+                    int batch, int Hkv, int D, int dtype, void *k_codes, void *k_scales, void *v_codes,
+                    void *v_scales, int cache_rows, void *stream);
+
+/* ddtree_compact into such a cache: for j = 0..n_accepted[s] the row dst_row[s] + j becomes tree row s*T + path[s][j].
+ * Rows dst_row[s] .. dst_row[s] + B must exist (DDTREE_ERR_ARG otherwise); entries of path outside 0 .. T-1
+ * are passed over. */
+int ddtree_q4_append(const void *k_tree, const void *v_tree, const int32_t *path,
+                     const int32_t *n_accepted, const int32_t *dst_row, int batch, int T, int B, int Hkv,
+                     int D, int dtype, void *k_codes, void *k_scales, void *v_codes, void *v_scales,
+                     int cache_rows, void *stream);
+
+/* The way back: rows from src_row[s] on become rows dst_offset[s] .. dst_offset[s+1] - 1 of k / v ([device]
+ * [dst_offset[batch], Hkv, D]; the two [host] arrays as in ddtree_q4_store). */
+int ddtree_q4_load(const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales,
+                   int cache_rows, const int32_t *src_row, const int32_t *dst_offset, int batch, int Hkv,
+                   int D, int dtype, void *k, void *v, void *stream);
+
+/*
  * Construction used by ddtree_build (Algorithm 1 defines the result; all constructions produce
  * it bit for bit).  DDTREE_BUILD_POPS runs the best-first pops one after the other on one
  * wavefront; DDTREE_BUILD_LEVELS finds the same N best prefixes (Proposition 2) as a set, depth by
@@ -308,7 +346,11 @@ int ddtree_build_handovers(unsigned int *count);
 #define DDTREE_KERNEL_ACCEPT_ARGMAX 5
 #define DDTREE_KERNEL_ACCEPT_WALK 6
 #define DDTREE_KERNEL_ATTN_GENERIC 7
-#define DDTREE_KERNEL_COUNT 8
+#define DDTREE_KERNEL_Q4_WRITE 8
+#define DDTREE_KERNEL_Q4_READ 9
+#define DDTREE_KERNEL_SAMPLE_SCAN 10
+#define DDTREE_KERNEL_SAMPLE_PICK 11
+#define DDTREE_KERNEL_COUNT 12
 int ddtree_profile_enable(unsigned kernel_mask, int capacity);
 int ddtree_profile_enable_every(unsigned kernel_mask, int capacity, int every);
 int ddtree_profile_reset(void);

@@ -34,6 +34,9 @@ _SIGNATURES = {
     "ddtree_compact": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp]),
     "ddtree_verify_attn_spans": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i,
                                       ctypes.c_float, _i, _vp, _vp, _sz, _vp]),
+    "ddtree_q4_store": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
+    "ddtree_q4_append": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
+    "ddtree_q4_load": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]),
     "ddtree_set_build_algorithm": (_i, [_i]),
     "ddtree_selftest_host": (_i, []),
     "ddtree_build_giveups": (_i, [ctypes.POINTER(ctypes.c_uint)]),
@@ -45,7 +48,8 @@ _SIGNATURES = {
 }
 
 KERNELS = {"topk_chunk": 0, "topk_merge": 1, "build": 2, "attn": 3, "attn_merge": 4,
-           "accept_argmax": 5, "accept_walk": 6, "attn_generic": 7}
+           "accept_argmax": 5, "accept_walk": 6, "attn_generic": 7, "q4_write": 8, "q4_read": 9,
+           "sample_scan": 10, "sample_pick": 11}
 
 
 class DDTreeError(RuntimeError):
@@ -304,6 +308,103 @@ def compact(k_tree, v_tree, path, n_accepted, dst_row, batch, T, B, Hkv, D, k_ca
     _check(load().ddtree_compact(_ptr(k_tree), _ptr(v_tree), _ptr(path), _ptr(n_accepted), dst_p, batch, T, B,
                                  Hkv, D, k_tree.element_size(), _ptr(k_cache), _ptr(v_cache), _stream()),
            "ddtree_compact")
+
+
+def _current(device):
+    """The calls launch on the current device's stream."""
+    if device != _device():
+        raise DDTreeError(f"the tensors are on device {device}, which is not the current one")
+
+
+class CacheQ4:
+    """A KV cache in 4 bits (format: ddtree.h): codes uint8 [Hkv, rows, D/2] and scales uint8 [Hkv, rows, D/32] of K and V.
+    CacheQ4.empty allocates one; the constructor takes the four tensors."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        for name, t in (("k_codes", k_codes), ("k_scales", k_scales), ("v_codes", v_codes), ("v_scales", v_scales)):
+            _dev(t, torch.uint8, name)
+        if k_codes.dim() != 3:
+            raise DDTreeError("k_codes: expected [Hkv, rows, D/2]")
+        Hkv, rows, half = k_codes.shape
+        if half % 16 != 0 or v_codes.shape != k_codes.shape or k_scales.shape != (Hkv, rows, half // 16) or \
+                v_scales.shape != k_scales.shape:
+            raise DDTreeError("codes are [Hkv, rows, D/2] and scales [Hkv, rows, D/32], D a multiple of 32")
+        if len({t.device for t in (k_codes, k_scales, v_codes, v_scales)}) != 1:
+            raise DDTreeError("the tensors of a cache are on one device")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.Hkv, self.rows, self.D, self.device = Hkv, rows, 2 * half, k_codes.get_device()
+        self.ptrs = (_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
+
+    @classmethod
+    def empty(cls, rows, Hkv, D, device="cuda"):
+        def bytes_(width):
+            return torch.empty((Hkv, rows, width), dtype=torch.uint8, device=device)
+        return cls(bytes_(D // 2), bytes_(D // 32), bytes_(D // 2), bytes_(D // 32))
+
+
+_ROW_DTYPE = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32}
+
+
+def _rows(t, cache, what):
+    """A tensor of K or V rows that goes with the cache; its DTYPE_*."""
+    dtype = _ROW_DTYPE.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if dtype is None or not t.is_cuda or not t.is_contiguous() or t.dim() != 3 or t.shape[1] != cache.Hkv or \
+            t.shape[2] != cache.D or t.get_device() != cache.device:
+        raise DDTreeError(f"{what}: expected a contiguous bfloat16 or float32 tensor [rows, {cache.Hkv}, {cache.D}] on the cache's device")
+    _current(cache.device)
+    return dtype
+
+
+def q4_store(k, v, src_offset, dst_row, cache, defer=False):
+    """Prompts into the cache: rows src_offset[s] .. src_offset[s+1] - 1 of k / v [rows, Hkv, D] become the rows from
+    dst_row[s] on (host int32 sequences of batch+1 and batch entries)."""
+    dtype = _rows(k, cache, "k")
+    if _rows(v, cache, "v") != dtype or v.shape[0] != k.shape[0]:
+        raise DDTreeError("k and v differ in rows or dtype")
+    batch = len(dst_row)
+    off, off_p = _host_i32(src_offset, batch + 1, "src_offset must have one entry more than dst_row")
+    dst, dst_p = _host_i32(dst_row, batch, "dst_row must be one-dimensional")
+    if batch and int(off[-1]) > k.shape[0]:
+        raise DDTreeError("src_offset names rows past the end of k and v")
+    args = (_ptr(k), _ptr(v), off_p, dst_p, batch, cache.Hkv, cache.D, dtype, *cache.ptrs, cache.rows, _stream())
+    run = _call("ddtree_q4_store", args, cache, defer)
+    return _keepalive(run, off, dst, k, v) if defer else run
+
+
+def q4_append(k_tree, v_tree, path, n_accepted, dst_row, batch, T, B, cache, defer=False):
+    """compact() into a 4-bit cache: the accepted tree rows are quantised behind each sequence."""
+    dtype = _rows(k_tree, cache, "k_tree")
+    if _rows(v_tree, cache, "v_tree") != dtype or v_tree.shape[0] != batch * T or k_tree.shape[0] != batch * T:
+        raise DDTreeError("k_tree and v_tree: expected batch*T rows of one dtype")
+    _dev(path, torch.int32, "path")
+    _dev(n_accepted, torch.int32, "n_accepted")
+    if path.numel() != batch * (B + 1) or n_accepted.numel() != batch:
+        raise DDTreeError("path must be [batch, B+1] and n_accepted [batch]")
+    dst, dst_p = _host_i32(dst_row, batch, "dst_row must have batch entries")
+    args = (_ptr(k_tree), _ptr(v_tree), _ptr(path), _ptr(n_accepted), dst_p, batch, T, B, cache.Hkv, cache.D, dtype,
+            *cache.ptrs, cache.rows, _stream())
+    run = _call("ddtree_q4_append", args, cache, defer)
+    return _keepalive(run, dst) if defer else run
+
+
+def q4_load(cache, src_row, dst_offset, dtype=torch.bfloat16, out=None, defer=False):
+    """Rows of the cache as tensors (k, v) [dst_offset[batch], Hkv, D] of dtype bfloat16 or float32: sequence s gives its
+    rows from src_row[s] on as rows dst_offset[s] .. dst_offset[s+1] - 1."""
+    batch = len(src_row)
+    src, src_p = _host_i32(src_row, batch, "src_row must be one-dimensional")
+    off, off_p = _host_i32(dst_offset, batch + 1, "dst_offset must have one entry more than src_row")
+    if out is None:
+        if dtype not in _ROW_DTYPE:
+            raise DDTreeError("dtype: expected torch.bfloat16 or torch.float32")
+        k = torch.empty((int(off[-1]), cache.Hkv, cache.D), dtype=dtype, device=cache.k_codes.device)
+        out = k, torch.empty_like(k)
+    k, v = out
+    code = _rows(k, cache, "k")
+    if _rows(v, cache, "v") != code or min(k.shape[0], v.shape[0]) < int(off[-1]):
+        raise DDTreeError("k and v differ in dtype, or have fewer rows than dst_offset names")
+    args = (*cache.ptrs, cache.rows, src_p, off_p, batch, cache.Hkv, cache.D, code, _ptr(k), _ptr(v), _stream())
+    run = _call("ddtree_q4_load", args, out, defer)
+    return _keepalive(run, src, off) if defer else run
 
 
 BUILD_AUTO, BUILD_POPS, BUILD_LEVELS = 0, 1, 2

@@ -54,6 +54,8 @@ bool attn_mfma_shape(int dtype, int D, int Hkv);
 bool attn_rows_fit(int T, int Hq, int Hkv);  // the query rows of a KV head are counted in 32 bits
 // scratch: bytes at hand.
 AttnPlan attn_plan(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch);
+bool q4_cache_ok(const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales, int cache_rows,
+                 int Hkv, int D);
 bool attn_lacks_scratch(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch);
 
 // ---- attn_wave_kernel ----
@@ -235,6 +237,16 @@ __device__ __forceinline__ uint32_t f2h_pair(float lo, float hi)
 {
     const f16x2 h = {(_Float16)lo, (_Float16)hi};
     return __builtin_bit_cast(uint32_t, h);
+}
+
+// Eight elements of a 4-bit cache (one word of codes, element 0 in the lowest bits) as packed bf16 pairs, exactly; scale:
+// their block's power of two, its byte moved to the exponent (255: the pairs are NaN).
+__device__ __forceinline__ void q4_decode8(uint32_t codes, float scale, uint32_t (&w)[4])
+{
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
 }
 
 // Compile-time loop: f(IC<B>{}), ..., f(IC<E-1>{}); the index is a constant expression inside f,
