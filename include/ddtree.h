@@ -288,6 +288,18 @@ int ddtree_q4_load(const void *k_codes, const void *k_scales, const void *v_code
                    int D, int dtype, void *k, void *v, void *stream);
 
 /*
+ * ddtree_verify_attn_spans over a 4-bit cache: sequence s owns its rows kv_start[s] .. kv_start[s] + kv_len[s] - 1
+ * (below cache_rows), whose keys and values are what the codes stand for; the tree rows are tensors of dtype, as there.
+ * T = 1 with the one bit of the mask set is a plain decoding step: the token sees the cache and itself.
+ * Arguments otherwise, precision and workspace as in ddtree_verify_attn; D a multiple of 32.
+ */
+int ddtree_verify_attn_q4(const void *q, const void *k_codes, const void *k_scales, const void *v_codes,
+                          const void *v_scales, int cache_rows, const void *k_tree, const void *v_tree,
+                          const uint64_t *ancestor_mask, const int32_t *kv_start, const int32_t *kv_len,
+                          int batch, int T, int Hq, int Hkv, int D, float softmax_scale, int dtype,
+                          void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Construction used by ddtree_build (Algorithm 1 defines the result; all constructions produce
  * it bit for bit).  DDTREE_BUILD_POPS runs the best-first pops one after the other on one
  * wavefront; DDTREE_BUILD_LEVELS finds the same N best prefixes (Proposition 2) as a set, depth by

@@ -37,6 +37,8 @@ _SIGNATURES = {
     "ddtree_q4_store": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "ddtree_q4_append": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "ddtree_q4_load": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]),
+    "ddtree_verify_attn_q4": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i,
+                                   ctypes.c_float, _i, _vp, _vp, _sz, _vp]),
     "ddtree_set_build_algorithm": (_i, [_i]),
     "ddtree_selftest_host": (_i, []),
     "ddtree_build_giveups": (_i, [ctypes.POINTER(ctypes.c_uint)]),
@@ -405,6 +407,30 @@ def q4_load(cache, src_row, dst_offset, dtype=torch.bfloat16, out=None, defer=Fa
     args = (*cache.ptrs, cache.rows, src_p, off_p, batch, cache.Hkv, cache.D, code, _ptr(k), _ptr(v), _stream())
     run = _call("ddtree_q4_load", args, out, defer)
     return _keepalive(run, src, off) if defer else run
+
+
+def verify_attn_q4(q, cache, k_tree, v_tree, ancestor_mask, kv_start, kv_len, batch, T, Hq, Hkv, D, softmax_scale, dtype, ws,
+                   out=None, defer=False):
+    """verify_attn_spans over a 4-bit cache (CacheQ4); T = 1 is a plain decoding step."""
+    if (cache.Hkv, cache.D) != (Hkv, D):
+        raise DDTreeError("the cache has other KV heads or another head size")
+    for name, t, heads in (("q", q, Hq), ("k_tree", k_tree, Hkv), ("v_tree", v_tree, Hkv)):
+        _dev(t, torch.bfloat16 if dtype == DTYPE_BF16 else torch.float32, name)
+        if t.numel() != batch * T * heads * D or t.get_device() != cache.device:
+            raise DDTreeError(f"{name}: expected [batch*T, {heads}, {D}] on the cache's device")
+    _dev(ancestor_mask, torch.int64, "ancestor_mask")
+    if ancestor_mask.numel() != batch * T * ((T + 63) // 64):
+        raise DDTreeError("ancestor_mask must be [batch, T, ceil(T/64)]")
+    _current(cache.device)
+    start, start_p = _host_i32(kv_start, batch, "kv_start and kv_len must have batch entries each")
+    length, length_p = _host_i32(kv_len, batch, "kv_start and kv_len must have batch entries each")
+    if out is None:
+        out = torch.empty_like(q)
+    p, n = _ws(ws)
+    args = (_ptr(q), *cache.ptrs, cache.rows, _ptr(k_tree), _ptr(v_tree), _ptr(ancestor_mask), start_p, length_p, batch, T,
+            Hq, Hkv, D, softmax_scale, dtype, _ptr(out), p, n, _stream())
+    run = _call("ddtree_verify_attn_q4", args, out, defer)
+    return _keepalive(run, start, length, cache) if defer else run
 
 
 BUILD_AUTO, BUILD_POPS, BUILD_LEVELS = 0, 1, 2

@@ -90,19 +90,23 @@ struct AttnTailArgs {
     int32_t T, Hq, Hkv, group_size;
     uint32_t g_magic;
     float scale_log2e;
+    AttnQ4Cache c4;
 };
 static_assert(WaveShape<kHD, 1>::threads == kAttnThreads && WaveShape<kHD, 1>::lds_bytes <= kAttnLdsBytes,
               "a tail block runs in a workgroup of this kernel");
 
 // WIDE: partial results are fp32 rows.  (A variant of its own: as a branch of the epilogue it cost the calls with
 // fp16 partials 0.45 us, 47.15 -> 47.6 at 257 nodes x 8192 keys.)
-template <bool WIDE>
-__global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,
+// Q4: the cache holds 4-bit codes.  A cache tile is then 4 KB of codes and 256 B of scales for K and as much for V: thread t
+// loads one block of 32 elements (K: the first half of the threads, V: the second) one step ahead of its use, and
+// writes it to the ring as bf16, which from there on is what the loads of a bf16 cache leave.
+template <bool WIDE, bool Q4>
+__device__ __forceinline__ void attn_mfma_body(
+                      const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,
                       const uint16_t *__restrict__ v_cache, const uint16_t *__restrict__ k_tree,
                       const uint16_t *__restrict__ v_tree, const uint64_t *__restrict__ mask,
-                      AttnMainArgs args, int T, int Hq, int Hkv, float scale_log2e,
-                      uint16_t *__restrict__ out, void *__restrict__ part, float2 *__restrict__ lse)
+                      const AttnMainArgs &args, int T, int Hq, int Hkv, float scale_log2e,
+                      uint16_t *__restrict__ out, void *__restrict__ part, float2 *__restrict__ lse, const AttnQ4Cache &c4)
 {
     // LDS: kAttnStages stages of {K tile, V tile}, filled by direct global->LDS loads.  One wave
     // instruction writes 64 x 16 B contiguously, but every lane may fetch any 16-byte chunk, so
@@ -136,10 +140,10 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
     if (!attn_main_item(args, (int)blockIdx.x, T, item)) return;
     if (item.tail) {
         const AttnTailArgs tail{q, k_cache, v_cache, k_tree, v_tree, mask, out, part, lse, T, Hq, Hkv,
-                                args.group_size, args.g_magic, scale_log2e};
+                                args.group_size, args.g_magic, scale_log2e, c4};
         const AttnWaveItem rows{item.seq, item.hk, 0, item.split, item.splits, item.ranges, item.first_slot, item.kv_start,
                                 item.kv_len, item.m0, item.m_end, item.n_cache, item.t_begin, item.t_end};
-        attn_wave_rows<kHD, 1, WIDE>(tail, rows);
+        attn_wave_rows<kHD, 1, WIDE, Q4>(tail, rows);
         return;
     }
     const int seq = item.seq, hk = item.hk, split = item.split, splits = item.splits;
@@ -174,8 +178,8 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
     // first cache row and first tree row of this (sequence, kv head), as byte addresses; a tile is
     // kKT consecutive keys, tile_bytes apart (the cache bases are formed but never used when the
     // sequence has no cache rows)
-    const unsigned char *const kc0 = reinterpret_cast<const unsigned char *>(k_cache) + ((size_t)L0 * Hkv + hk) * (kHD * 2);
-    const unsigned char *const vc0 = reinterpret_cast<const unsigned char *>(v_cache) + ((size_t)L0 * Hkv + hk) * (kHD * 2);
+    const unsigned char *const kc0 = Q4 ? nullptr : reinterpret_cast<const unsigned char *>(k_cache) + ((size_t)L0 * Hkv + hk) * (kHD * 2);
+    const unsigned char *const vc0 = Q4 ? nullptr : reinterpret_cast<const unsigned char *>(v_cache) + ((size_t)L0 * Hkv + hk) * (kHD * 2);
     const unsigned char *const kt0 = reinterpret_cast<const unsigned char *>(k_tree) + ((size_t)seq * T * Hkv + hk) * (kHD * 2);
     const unsigned char *const vt0 = reinterpret_cast<const unsigned char *>(v_tree) + ((size_t)seq * T * Hkv + hk) * (kHD * 2);
     const uint32_t tile_bytes = (uint32_t)kKT * row_bytes;
@@ -204,11 +208,11 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
         // (24-bit multiplies: a row index below 64 times a row pitch below 2^24 -- the full multiply-add
         // leaves its result in a register pair, and six such pairs were kept through the kernel)
         k_src[i] = __umul24((uint32_t)min(rk, kKT - 1), row_bytes) + (ck == 16 ? 0 : ck) * 16;  // padding slot: any chunk
-        const int rv = u >> 4, cv = (u & 15) ^ ((rv & 3) << 2);  // slot (row, position) holds chunk position ^ 4 (row & 3)
+        const int rv = u >> 4, cv = (u & 15) ^ ((rv & 3) << 2) ^ (Q4 ? rv & 3 : 0);  // slot (row, position) holds chunk position ^ 4 (row & 3)
         v_src[i] = __umul24((uint32_t)min(rv, kKT - 1), row_bytes) + cv * 16;
     }
     auto issue_tile = [&](int tt, int stage) __attribute__((always_inline)) {
-        const bool cache = tt < n_cache_tiles;
+        const bool cache = !Q4 && tt < n_cache_tiles;  // (Q4: called for tiles of the tree only)
         const int tl = cache ? tt : tt - n_cache_tiles;
         const uint64_t toff = (uint64_t)(uint32_t)tl * tile_bytes;
         const unsigned char *kp = (cache ? kc0 : kt0) + toff;
@@ -245,7 +249,7 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
                     dma(kp, __umul24((uint32_t)min(r, valid_ - 1), row_bytes) + (c == 16 ? 0 : c) * 16, st + blk * 1024);
                 }
                 if (blk < 16) {
-                    const int r = u >> 4, c = (u & 15) ^ ((r & 3) << 2);
+                    const int r = u >> 4, c = (u & 15) ^ ((r & 3) << 2) ^ (Q4 ? r & 3 : 0);
                     dma(vp, __umul24((uint32_t)min(r, valid_ - 1), row_bytes) + c * 16, st + kKTileBytes + blk * 1024);
                 }
             }
@@ -263,12 +267,66 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
 
     // Everything in LDS is addressed from a 256-byte boundary: the V operand addresses below take
     // an exclusive-or on bits 6 and 7.
+    // Q4: the block that this thread brings of a cache tile, of key q4_row its elements 32 q4_blk on.  K goes to the padded
+    // rows; of V's 64-byte blocks, at block ^ (row & 3) as everywhere, the four chunks sit at chunk ^ (row & 3), so that the
+    // 16 lanes that write chunk c of four rows' blocks do not meet on a bank.
+    const uint32_t q4_tid = (uint32_t)tid & 255u;
+    const bool q4_v = Q4 && wave_u >= kWaves / 2;
+    const uint8_t *q4_codes = nullptr, *q4_scales = nullptr;
+    u32x4 q4_code = (u32x4){0u, 0u, 0u, 0u};
+    uint32_t q4_scale = 0u;
+    if constexpr (Q4) {
+        const size_t row0 = (size_t)hk * c4.rows + L0;
+        q4_codes = (q4_v ? c4.v_codes : c4.k_codes) + row0 * (kHD / 2);
+        q4_scales = (q4_v ? c4.v_scales : c4.k_scales) + row0 * (kHD / 32);
+    }
+    auto q4_fetch = [&](int tt) __attribute__((always_inline)) {
+        const uint64_t key = (uint64_t)(uint32_t)tt * kKT;
+        const uint32_t r = min((int)(q4_tid >> 2), L - 1 - (int)key);  // (rows past the end repeat the last)
+        const uint32_t at = r * 4 + (q4_tid & 3);
+        q4_code = *reinterpret_cast<const u32x4 *>(q4_codes + key * (kHD / 2) + at * 16);
+        q4_scale = q4_scales[key * (kHD / 32) + at];
+    };
+    auto q4_put = [&](int stage, const u32x4 &code, uint32_t scale_byte) __attribute__((always_inline)) {
+        int t = (int)threadIdx.x;
+        asm volatile("" : "+v"(t));
+        const uint32_t r = (uint32_t)(t >> 2) & 63u, blk = (uint32_t)t & 3u;
+        const uint32_t x = q4_v ? r & 3u : 0u;
+        const uint32_t base = (((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem_raw + 255u) & ~255u) +
+                              (uint32_t)(stage * kStageBytes) + (q4_v ? (uint32_t)kKTileBytes + r * kVRowBytes : r * kKRowBytes) + ((blk ^ x) << 6);
+        const float scale = __uint_as_float(scale_byte << 23);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint32_t w[4];
+            q4_decode8(code[c], scale, w);
+            asm volatile("ds_write_b128 %0, %1" ::"v"(base + (((uint32_t)c ^ x) << 4)), "v"((u32x4){w[0], w[1], w[2], w[3]}) : "memory");
+        }
+    };
+    // the first three tiles of the key range; a third one of the cache stays in registers
+    auto q4_first = [&]() __attribute__((always_inline)) {
+        const int cached = max(0, min(3, min(n_tiles, n_cache_tiles - t_begin)));
+        u32x4 code[2];
+        uint32_t scale[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i < cached) q4_fetch(t_begin + i);
+            code[i] = q4_code, scale[i] = q4_scale;
+        }
+        if (cached > 2) q4_fetch(t_begin + 2);
+        for (int i = cached; i < min(3, n_tiles); ++i) issue_tile(t_begin + i, i);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (i < cached) q4_put(i, code[i], scale[i]);
+    };
+
     const uint32_t lds_base = ((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem_raw + 255u) & ~255u;
 
     // ---- the first requests: the first key tile, the queries and mask words, two more key tiles.
     //      Vector memory operations complete in order, so the wait for "all but the last tile
     //      requested" further down also covers the queries and the mask words. ----
-    if (n_tiles > 0) issue_tile(t_begin, 0);
+    if constexpr (!Q4) {
+        if (n_tiles > 0) issue_tile(t_begin, 0);
+    }
     __builtin_amdgcn_sched_barrier(0);
     // Q^T operand: lane holds Q[row][16*ks + 8*half .. +8]
     bf16x8 qreg[8];
@@ -291,8 +349,12 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
         for (int i = 0; i < kMaskStages; ++i) mword[i] = (rv && i < n_stage) ? mask_row(nd)[tb0 + i] : 0ull;
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (n_tiles > 1) issue_tile(t_begin + 1, 1);
-    if (n_tiles > 2) issue_tile(t_begin + 2, 2);
+    if constexpr (!Q4) {
+        if (n_tiles > 1) issue_tile(t_begin + 1, 1);
+        if (n_tiles > 2) issue_tile(t_begin + 2, 2);
+    } else {
+        q4_first();
+    }
     __builtin_amdgcn_sched_barrier(0);
     // LDS address of this lane's row in the staged mask words (both half-waves of a row read the
     // same word); tree tile tb0 + i is kMaskStageBytes * i further on
@@ -308,7 +370,8 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
     // V: row 4*half + lm/4 (+16*kstep, +8), dims 32*db + 16*dim16 + 4*(lm%4); the 64-byte block db of
     // a row sits at position db ^ (row & 3), and row & 3 = lm / 4 for every row this lane reads: the
     // base points at block (row & 3), the position of db = 0, and a read takes base ^ (db * 64)
-    const int v_base = kKTileBytes + (4 * half + (lm >> 2)) * kVRowBytes + ((lm >> 2) << 6) + 32 * dim16 + 8 * (lm & 3);
+    const int v_base = kKTileBytes + (4 * half + (lm >> 2)) * kVRowBytes + ((lm >> 2) << 6) +
+                       (!Q4 ? 32 * dim16 + 8 * (lm & 3) : (((2 * dim16 + ((lm & 3) >> 1)) ^ (lm >> 2)) << 4) + 8 * (lm & 1));
     static_assert((kKTileBytes & 0xFF) == 0 && (kStageBytes & 0xFF) == 0 && (kVRowBytes & 0xFF) == 0,
                   "bits 6 and 7 of a V operand address come from the block position alone");
 
@@ -481,11 +544,20 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
         // (its K operands are requested one sub-tile ahead), tile it+2 is in flight and tile it+3
         // is requested into the stage that tile it-1 has just left.
         if (pass > 0) {  // (the first pass's tiles were requested at the top of the kernel)
-            if (n_tiles > 0) issue_tile(t_begin, 0);
-            if (n_tiles > 1) issue_tile(t_begin + 1, 1);
-            if (n_tiles > 2) issue_tile(t_begin + 2, 2);
+            if constexpr (Q4) {
+                q4_first();
+            } else {
+                if (n_tiles > 0) issue_tile(t_begin, 0);
+                if (n_tiles > 1) issue_tile(t_begin + 1, 1);
+                if (n_tiles > 2) issue_tile(t_begin + 2, 2);
+            }
         }
-        tiles_in_flight(n_tiles > 2 ? 1 : 0);  // tiles 0 and 1 have landed
+        if constexpr (Q4) {
+            vm_wait<0>();  // (tiles of the tree, in the workgroups that begin with it or soon come to it)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        } else {
+            tiles_in_flight(n_tiles > 2 ? 1 : 0);  // tiles 0 and 1 have landed
+        }
         __syncthreads();
         if (wave_active && n_tiles > 0) {
             // S(0) on its own, then the operands the first step expects: K(1), and V(0) standing in
@@ -521,11 +593,26 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
                 // Tile it+1 has landed (this wave's share; the barrier makes it everyone's) and
                 // nobody reads tile it-1 any more: its stage takes tile it+3.
                 if (wave_active) lds_wait_all(kbuf, vbuf);
-                tiles_in_flight(it + 2 < n_tiles ? 1 : 0);
+                if constexpr (Q4) {
+                    // (a cache tile's rows were written by LDS instructions; a tile of the tree that follows the last one was
+                    // requested behind the codes of its predecessor)
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    if (t + 1 >= n_cache_tiles) tiles_in_flight(it + 2 < n_tiles ? 1 : 0);
+                } else {
+                    tiles_in_flight(it + 2 < n_tiles ? 1 : 0);
+                }
                 __syncthreads();
             }
             auto request = [&]() __attribute__((always_inline)) {
-                if (it + 3 < n_tiles) issue_tile(t + 3, (it + 3) & (kAttnStages - 1));
+                if constexpr (Q4) {
+                    if (it + 2 < n_tiles && t + 2 < n_cache_tiles) q4_put((it + 2) & (kAttnStages - 1), q4_code, q4_scale);
+                    if (it + 3 < n_tiles) {
+                        if (t + 3 < n_cache_tiles) q4_fetch(t + 3);
+                        else issue_tile(t + 3, (it + 3) & (kAttnStages - 1));
+                    }
+                } else {
+                    if (it + 3 < n_tiles) issue_tile(t + 3, (it + 3) & (kAttnStages - 1));
+                }
             };
             if (!wave_active) request();
             if (wave_active) {
@@ -666,6 +753,25 @@ void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict
     }
 }
 
+template <bool WIDE>
+__global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void attn_mfma_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,
+                      const uint16_t *__restrict__ v_cache, const uint16_t *__restrict__ k_tree,
+                      const uint16_t *__restrict__ v_tree, const uint64_t *__restrict__ mask,
+                      AttnMainArgs args, int T, int Hq, int Hkv, float scale_log2e,
+                      uint16_t *__restrict__ out, void *__restrict__ part, float2 *__restrict__ lse)
+{
+    attn_mfma_body<WIDE, false>(q, k_cache, v_cache, k_tree, v_tree, mask, args, T, Hq, Hkv, scale_log2e, out, part, lse, AttnQ4Cache{});
+}
+template <bool WIDE>
+__global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void attn_mfma_q4_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_tree, const uint16_t *__restrict__ v_tree,
+                         const uint64_t *__restrict__ mask, AttnMainArgs args, int T, int Hq, int Hkv, float scale_log2e,
+                         uint16_t *__restrict__ out, void *__restrict__ part, float2 *__restrict__ lse, AttnQ4Cache c4)
+{
+    attn_mfma_body<WIDE, true>(q, nullptr, nullptr, k_tree, v_tree, mask, args, T, Hq, Hkv, scale_log2e, out, part, lse, c4);
+}
+
 // Merge of the split-KV partials: out = sum_s 2^(lse_s - max) O_s / sum_s 2^(lse_s - max).
 // Partials are normalised per split and stored as fp32, or as fp16 relative to the largest magnitude of
 // the row, which travels beside the row's log2-sum-exp (eps 2^-11 is below the bf16 rounding of the
@@ -772,12 +878,31 @@ __device__ __forceinline__ void st_elem(uint16_t *p, float v)
     *p = __builtin_bit_cast(unsigned short, b);
 }
 
-template <typename TIO>
-__global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
+// eight elements of a 4-bit row from element c on, and one element
+__device__ __forceinline__ void q4_elem8(const uint8_t *codes, const uint8_t *scales, int c, float (&o)[8])
+{
+    uint32_t w[4];
+    q4_decode8(*reinterpret_cast<const uint32_t *>(codes + c / 2), __uint_as_float((uint32_t)scales[c / 32] << 23), w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o[2 * i] = __uint_as_float(w[i] << 16);
+        o[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ float q4_elem(const uint8_t *codes, const uint8_t *scales, int c)
+{
+    const uint32_t code = (uint32_t)codes[c / 2] >> (4 * (c & 1));
+    const uint32_t pair = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, __uint_as_float((uint32_t)scales[c / 32] << 23), 0));
+    return __uint_as_float(pair << 16);
+}
+
+// (Q4: the cache holds 4-bit codes, D is a multiple of 32)
+template <typename TIO, bool Q4>
+__device__ __forceinline__ void attn_generic_body(
     const TIO *__restrict__ q, const TIO *__restrict__ k_cache, const TIO *__restrict__ v_cache,
     const TIO *__restrict__ k_tree, const TIO *__restrict__ v_tree,
-    const uint64_t *__restrict__ mask, AttnGenericArgs args, int T, int Hq, int Hkv, int D, float scale,
-    TIO *__restrict__ out)
+    const uint64_t *__restrict__ mask, const AttnGenericArgs &args, int T, int Hq, int Hkv, int D, float scale,
+    TIO *__restrict__ out, const AttnQ4Cache &c4)
 {
     __shared__ float s_q[256];
     __shared__ float s_p[kGenThreads];
@@ -807,7 +932,23 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
         float s = -INFINITY;
         const TIO *krow = nullptr;
         if (j < L) {
-            krow = k_cache + ((size_t)(L0 + j) * Hkv + hk) * D;
+            if constexpr (Q4) {
+                const size_t row = (size_t)hk * c4.rows + L0 + j;
+                const uint8_t *const codes = c4.k_codes + row * (D / 2), *const scales = c4.k_scales + row * (D / 32);
+                float dot = 0.0f;
+                for (int c = 0; c < D; c += 16) {
+                    float k0[8], k1[8];
+                    q4_elem8(codes, scales, c, k0);
+                    q4_elem8(codes, scales, c + 8, k1);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) dot = fmaf(s_q[c + u], k0[u], dot);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) dot = fmaf(s_q[c + 8 + u], k1[u], dot);
+                }
+                s = dot * scale;
+            } else {
+                krow = k_cache + ((size_t)(L0 + j) * Hkv + hk) * D;
+            }
         } else if (j < total) {
             const int jt = j - L;
             if ((mrow[jt >> 6] >> (jt & 63)) & 1ull)
@@ -865,15 +1006,24 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
                 return jj < L ? v_cache + ((size_t)(L0 + jj) * Hkv + hk) * D
                               : v_tree + (((size_t)seq * T + (jj - L)) * Hkv + hk) * D;
             };
+            auto velem = [&](int jj) -> float {
+                if constexpr (Q4) {
+                    if (jj < L) {
+                        const size_t row = (size_t)hk * c4.rows + L0 + jj;
+                        return q4_elem(c4.v_codes + row * (D / 2), c4.v_scales + row * (D / 32), gd);
+                    }
+                }
+                return ld_elem(vrow(jj) + gd);
+            };
             int t = gg;
             for (; t + 15 * groups < cnt; t += 16 * groups) {
                 float vv[16];
 #pragma unroll
-                for (int u = 0; u < 16; ++u) vv[u] = ld_elem(vrow(j0 + t + u * groups) + gd);
+                for (int u = 0; u < 16; ++u) vv[u] = velem(j0 + t + u * groups);
 #pragma unroll
                 for (int u = 0; u < 16; ++u) acc = fmaf(s_p[t + u * groups], vv[u], acc);
             }
-            for (; t < cnt; t += groups) acc = fmaf(s_p[t], ld_elem(vrow(j0 + t) + gd), acc);
+            for (; t < cnt; t += groups) acc = fmaf(s_p[t], velem(j0 + t), acc);
         }
         __syncthreads();
     }
@@ -887,10 +1037,29 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
     }
 }
 
+template <typename TIO>
+__global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
+    const TIO *__restrict__ q, const TIO *__restrict__ k_cache, const TIO *__restrict__ v_cache,
+    const TIO *__restrict__ k_tree, const TIO *__restrict__ v_tree,
+    const uint64_t *__restrict__ mask, AttnGenericArgs args, int T, int Hq, int Hkv, int D, float scale,
+    TIO *__restrict__ out)
+{
+    attn_generic_body<TIO, false>(q, k_cache, v_cache, k_tree, v_tree, mask, args, T, Hq, Hkv, D, scale, out, AttnQ4Cache{});
+}
+template <typename TIO>
+__global__ __launch_bounds__(kGenThreads) void attn_generic_q4_kernel(
+    const TIO *__restrict__ q, const TIO *__restrict__ k_tree, const TIO *__restrict__ v_tree,
+    const uint64_t *__restrict__ mask, AttnGenericArgs args, int T, int Hq, int Hkv, int D, float scale,
+    TIO *__restrict__ out, AttnQ4Cache c4)
+{
+    attn_generic_body<TIO, true>(q, nullptr, nullptr, k_tree, v_tree, mask, args, T, Hq, Hkv, D, scale, out, c4);
+}
+
 }  // namespace ddt
 
-static int verify_attn_impl(const void *q, const void *k_cache, const void *v_cache, const void *k_tree,
-                            const void *v_tree, const uint64_t *ancestor_mask, const int32_t *kv_start,
+// c4: the cache in 4 bits, in the place of k_cache and v_cache.
+static int verify_attn_impl(const void *q, const void *k_cache, const void *v_cache, const ddt::AttnQ4Cache *c4,
+                            const void *k_tree, const void *v_tree, const uint64_t *ancestor_mask, const int32_t *kv_start,
                             const int32_t *kv_len, int batch, int T, int Hq, int Hkv, int D,
                             float softmax_scale, int dtype, void *out, void *workspace,
                             size_t workspace_bytes, void *stream)
@@ -912,7 +1081,12 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
             return DDTREE_ERR_ARG;
         sum_L += kv_len[s];
     }
-    if (sum_L > 0 && (!k_cache || !v_cache)) return DDTREE_ERR_ARG;
+    if (!c4 && sum_L > 0 && (!k_cache || !v_cache)) return DDTREE_ERR_ARG;
+    if (c4) {
+        if (!q4_cache_ok(c4->k_codes, c4->k_scales, c4->v_codes, c4->v_scales, c4->rows, Hkv, D)) return DDTREE_ERR_ARG;
+        for (int s = 0; s < batch; ++s)
+            if ((long long)kv_start[s] + kv_len[s] > c4->rows) return DDTREE_ERR_ARG;
+    }
     hipStream_t st = as_stream(stream);
 
     if (attn_mfma_shape(dtype, D, Hkv)) {
@@ -933,7 +1107,7 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
             most = std::max(most, p.seq[i].ranges);
         }
         if (p.row_blocks > 0) {
-            AttnWaveArgs args;
+            AttnWaveQ4Args args;
             if (!attn_wave_args(args, p, kv_start, kv_len, batch, T, Hq, Hkv)) return DDTREE_ERR_ARG;
             args.q = static_cast<const uint16_t *>(q);
             args.k_cache = static_cast<const uint16_t *>(k_cache);
@@ -948,11 +1122,22 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
             args.Hq = Hq;
             args.Hkv = Hkv;
             args.scale_log2e = softmax_scale * kLog2e;
-            if (!attn_wave_launch(args, D, p.row_blocks, p.wide, st)) return DDTREE_ERR_HIP;
+            if (c4) args.c4 = *c4;
+            if (!(c4 ? attn_wave_launch_q4(args, D, p.row_blocks, p.wide, st) : attn_wave_launch(args, D, p.row_blocks, p.wide, st)))
+                return DDTREE_ERR_HIP;
         } else {
             AttnMainArgs args;
             if (!attn_main_args(args, p, kv_start, kv_len, batch, T, Hq, Hkv)) return DDTREE_ERR_ARG;
-            static std::atomic<bool> lds_allowed[2];
+            static std::atomic<bool> lds_allowed[2], lds_allowed_q4[2];
+            if (c4) {
+                auto *kernel = p.wide ? attn_mfma_q4_kernel<true> : attn_mfma_q4_kernel<false>;
+                if (!allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kAttnLdsBytes, lds_allowed_q4[p.wide ? 1 : 0]))
+                    return DDTREE_ERR_HIP;
+                DDT_LAUNCH(DDTREE_KERNEL_ATTN, st, kernel, dim3((unsigned)args.grid), dim3(kAttnThreads), kAttnLdsBytes, st,
+                           static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_tree),
+                           static_cast<const uint16_t *>(v_tree), ancestor_mask, args, T, Hq, Hkv, softmax_scale * kLog2e,
+                           static_cast<uint16_t *>(out), part, lse, *c4);
+            } else {
             auto *kernel = p.wide ? attn_mfma_kernel<true> : attn_mfma_kernel<false>;
             if (!allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kAttnLdsBytes, lds_allowed[p.wide ? 1 : 0]))
                 return DDTREE_ERR_HIP;
@@ -961,6 +1146,7 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
                        static_cast<const uint16_t *>(v_cache), static_cast<const uint16_t *>(k_tree),
                        static_cast<const uint16_t *>(v_tree), ancestor_mask, args, T, Hq, Hkv,
                        softmax_scale * kLog2e, static_cast<uint16_t *>(out), part, lse);
+            }
         }
         if (most > 1) {
             const int rows_seq = T * Hq;
@@ -983,7 +1169,16 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
         args.kv_start[s] = kv_start[s];
         args.kv_len[s] = kv_len[s];
     }
-    if (dtype == DDTREE_DTYPE_FP32)
+    if (c4) {
+        if (dtype == DDTREE_DTYPE_FP32)
+            DDT_LAUNCH(DDTREE_KERNEL_ATTN_GENERIC, st, attn_generic_q4_kernel<float>, dim3(Hq, T, batch), dim3(kGenThreads), 0, st,
+                       static_cast<const float *>(q), static_cast<const float *>(k_tree), static_cast<const float *>(v_tree),
+                       ancestor_mask, args, T, Hq, Hkv, D, softmax_scale, static_cast<float *>(out), *c4);
+        else
+            DDT_LAUNCH(DDTREE_KERNEL_ATTN_GENERIC, st, attn_generic_q4_kernel<uint16_t>, dim3(Hq, T, batch), dim3(kGenThreads), 0, st,
+                       static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_tree), static_cast<const uint16_t *>(v_tree),
+                       ancestor_mask, args, T, Hq, Hkv, D, softmax_scale, static_cast<uint16_t *>(out), *c4);
+    } else if (dtype == DDTREE_DTYPE_FP32)
         DDT_LAUNCH(DDTREE_KERNEL_ATTN_GENERIC, st, attn_generic_kernel<float>, dim3(Hq, T, batch), dim3(kGenThreads), 0, st,
                            static_cast<const float *>(q), static_cast<const float *>(k_cache),
                            static_cast<const float *>(v_cache), static_cast<const float *>(k_tree),
@@ -1011,7 +1206,7 @@ extern "C" int ddtree_verify_attn(const void *q, const void *k_cache, const void
         start[s] = kv_offset[s];
         len[s] = kv_offset[s + 1] - kv_offset[s];
     }
-    return verify_attn_impl(q, k_cache, v_cache, k_tree, v_tree, ancestor_mask, start, len, batch, T, Hq,
+    return verify_attn_impl(q, k_cache, v_cache, nullptr, k_tree, v_tree, ancestor_mask, start, len, batch, T, Hq,
                             Hkv, D, softmax_scale, dtype, out, workspace, workspace_bytes, stream);
 }
 
@@ -1023,7 +1218,20 @@ extern "C" int ddtree_verify_attn_spans(const void *q, const void *k_cache, cons
                                         size_t workspace_bytes, void *stream)
 {
     if (batch < 1 || batch > DDTREE_MAX_BATCH) return DDTREE_ERR_ARG;
-    return verify_attn_impl(q, k_cache, v_cache, k_tree, v_tree, ancestor_mask, kv_start, kv_len, batch, T,
+    return verify_attn_impl(q, k_cache, v_cache, nullptr, k_tree, v_tree, ancestor_mask, kv_start, kv_len, batch, T,
                             Hq, Hkv, D, softmax_scale, dtype, out, workspace, workspace_bytes, stream);
 }
 
+
+extern "C" int ddtree_verify_attn_q4(const void *q, const void *k_codes, const void *k_scales, const void *v_codes,
+                                     const void *v_scales, int cache_rows, const void *k_tree, const void *v_tree,
+                                     const uint64_t *ancestor_mask, const int32_t *kv_start, const int32_t *kv_len,
+                                     int batch, int T, int Hq, int Hkv, int D, float softmax_scale, int dtype, void *out,
+                                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (batch < 1 || batch > DDTREE_MAX_BATCH) return DDTREE_ERR_ARG;
+    const ddt::AttnQ4Cache c4{static_cast<const uint8_t *>(k_codes), static_cast<const uint8_t *>(k_scales),
+                              static_cast<const uint8_t *>(v_codes), static_cast<const uint8_t *>(v_scales), cache_rows};
+    return verify_attn_impl(q, nullptr, nullptr, &c4, k_tree, v_tree, ancestor_mask, kv_start, kv_len, batch, T,
+                            Hq, Hkv, D, softmax_scale, dtype, out, workspace, workspace_bytes, stream);
+}

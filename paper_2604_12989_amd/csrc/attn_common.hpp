@@ -81,9 +81,18 @@ struct AttnWaveArgs {
     float scale_log2e;
     AttnWaveSeq seq[DDTREE_MAX_BATCH];   // (behind what every workgroup reads first)
 };
+// A 4-bit cache (format: cache_q4.hip), read where the others read k_cache and v_cache.
+struct AttnQ4Cache {
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int32_t rows;
+};
+struct AttnWaveQ4Args : AttnWaveArgs {
+    AttnQ4Cache c4;
+};
 bool attn_wave_args(AttnWaveArgs &args, const AttnPlan &p, const int32_t *kv_start, const int32_t *kv_len, int batch,
                     int T, int Hq, int Hkv);
 bool attn_wave_launch(const AttnWaveArgs &args, int D, int row_blocks, bool wide, hipStream_t st);
+bool attn_wave_launch_q4(const AttnWaveQ4Args &args, int D, int row_blocks, bool wide, hipStream_t st);
 
 struct AttnWaveItem {
     int seq, hk, grp, split, splits, ranges, first_slot, kv_start, kv_len;

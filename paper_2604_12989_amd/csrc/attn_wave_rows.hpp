@@ -29,8 +29,11 @@ struct WaveShape {
 };
 
 // What a workgroup does with its row group and key range.  Args: AttnWaveArgs, or what attn_mfma_kernel has; WIDE:
-// partial results are fp32 rows.
-template <int D, int RB, bool WIDE, class Args>
+// partial results are fp32 rows.  Q4: the cache holds 4-bit codes (args.c4).  A wave then takes the codes of its cache
+// sub-tiles, 4.25 KB at D = 128, into registers one sub-tile ahead.  Those of K become the operand of the first product as they are
+// (a lane loads half of its key's row, four exchanges between the half-waves give each lane the dims of its k-steps); those
+// of V, which the second product wants by columns, become bf16 rows in LDS for the transposing reads.
+template <int D, int RB, bool WIDE, bool Q4 = false, class Args>
 __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveItem &item)
 {
     using S = WaveShape<D, RB>;
@@ -84,8 +87,8 @@ __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveI
     const uint32_t *const mrow = mask32 + (size_t)div_by(min(r0 + (RB == 2 ? lane : l32), r1 - 1), G, args.g_magic) * W2;
 
     const uint32_t pitch = (uint32_t)Hkv * S::row_bytes;  // bytes between consecutive keys in global memory
-    const unsigned char *const kc0 = reinterpret_cast<const unsigned char *>(args.k_cache) + ((size_t)item.kv_start * Hkv + hk) * S::row_bytes;
-    const unsigned char *const vc0 = reinterpret_cast<const unsigned char *>(args.v_cache) + ((size_t)item.kv_start * Hkv + hk) * S::row_bytes;
+    const unsigned char *const kc0 = Q4 ? nullptr : reinterpret_cast<const unsigned char *>(args.k_cache) + ((size_t)item.kv_start * Hkv + hk) * S::row_bytes;
+    const unsigned char *const vc0 = Q4 ? nullptr : reinterpret_cast<const unsigned char *>(args.v_cache) + ((size_t)item.kv_start * Hkv + hk) * S::row_bytes;
     const unsigned char *const kt0 = reinterpret_cast<const unsigned char *>(args.k_tree) + ((size_t)seq * T * Hkv + hk) * S::row_bytes;
     const unsigned char *const vt0 = reinterpret_cast<const unsigned char *>(args.v_tree) + ((size_t)seq * T * Hkv + hk) * S::row_bytes;
     unsigned char *const ring = smem + wave * S::ring_bytes;
@@ -93,12 +96,15 @@ __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveI
     // LDS layout of a sub-tile: rows of D elements, 16-byte chunks moved about inside a row (or a pair
     // of rows for D = 64) so that neither the 16-byte K reads (a lane a row) nor the transposing V
     // reads (a half-wave four rows) meet on a bank.  K: chunk c of row r sits at c ^ (r & 15)
-    // (D = 64: c ^ (r / 2 & 7)); V: 64-byte block b at b ^ (r & 3) (D = 64: b ^ (r / 2 & 1)).
+    // (D = 64: c ^ (r / 2 & 7)); V: 64-byte block b at b ^ (r & 3) (D = 64: b ^ (r / 2 & 1)).  Q4: the four chunks of a block,
+    // which a lane writes one after the other, at c ^ (r & 3) of it (D = 64: c ^ (r / 2 & 3)), so that the 16 lanes
+    // that write four rows of four blocks (eight of two) do not meet either.
     const int d_row = lane / S::chunks, d_pos = lane % S::chunks;
     auto k_chunk = [&](int i) __attribute__((always_inline)) {  // source chunk of this lane's slot in load i
         return D == 128 ? d_pos ^ d_row ^ ((i & 3) * 4) : d_pos ^ (d_row >> 1) ^ ((i & 1) * 4);
     };
-    const int v_chunk = D == 128 ? d_pos ^ (d_row << 2) : d_pos ^ (((d_row >> 1) & 1) << 2);
+    const int v_chunk = (D == 128 ? d_pos ^ (d_row << 2) : d_pos ^ (((d_row >> 1) & 1) << 2)) ^
+                        (!Q4 ? 0 : D == 128 ? d_row & 3 : (d_row >> 1) & 3);
     constexpr int KV = D == 128 ? 4 : 2;  // distinct K source chunks of a lane
     uint32_t k_off[KV];
 #pragma unroll
@@ -137,12 +143,51 @@ __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveI
                                              (__attribute__((address_space(3))) void *)(ring + (i % NS) * S::stage_bytes + 2 * S::tile_bytes),
                                              4, 0, 0);
     };
-    if (n > 0) {
-        issue_mask(0);
-        issue(0, true);
-        issue(0, false);
+    // Q4: the first n4 of the wave's sub-tiles are the cache's
+    const int n4 = Q4 ? max(0, min(n, (min(n_cache, item.t_end) - item.t_begin - wave + NW - 1) / NW)) : 0;
+    constexpr int CW = D / 64;  // 16-byte loads of a lane for K, and for V
+    // (K: row l32, half of it; V: row d4_row + 16 j of the sub-tile, D = 64: d4_row, its block d4_blk)
+    const int d4_row = lane / (D / 32), d4_blk = lane % (D / 32);
+    u32x4 kc4[CW], vc4[CW];
+    uint32_t ks4 = 0u, vs4[CW];
+    const uint8_t *kq0 = nullptr, *ksc0 = nullptr, *vq0 = nullptr, *vsc0 = nullptr;
+    if constexpr (Q4) {
+        const size_t row0 = (size_t)hk * args.c4.rows + item.kv_start;
+        kq0 = args.c4.k_codes + row0 * (D / 2), ksc0 = args.c4.k_scales + row0 * (D / 32);
+        vq0 = args.c4.v_codes + row0 * (D / 2), vsc0 = args.c4.v_scales + row0 * (D / 32);
     }
-    if (NS > 1 && n > 1) {
+    auto load_k4 = [&](int i) __attribute__((always_inline)) {
+        const uint64_t t = (uint64_t)(uint32_t)(t_first + i * NW) * kSK;
+        const uint32_t r = min(l32, L - 1 - (int)t);  // (rows past the end repeat the last)
+        const uint8_t *p = kq0 + t * (D / 2), *q = ksc0 + t * (D / 32);
+#pragma unroll
+        for (int j = 0; j < CW; ++j) kc4[j] = *reinterpret_cast<const u32x4 *>(p + (r * (D / 2) + half * (D / 4) + j * 16));
+        if constexpr (D == 128) ks4 = *reinterpret_cast<const uint32_t *>(q + r * 4);
+        else ks4 = *reinterpret_cast<const uint16_t *>(q + r * 2);
+    };
+    auto load_v4 = [&](int i) __attribute__((always_inline)) {
+        const uint64_t t = (uint64_t)(uint32_t)(t_first + i * NW) * kSK;
+        const uint8_t *p = vq0 + t * (D / 2), *q = vsc0 + t * (D / 32);
+#pragma unroll
+        for (int j = 0; j < CW; ++j) {
+            const uint32_t r = min(d4_row + 16 * j, L - 1 - (int)t);
+            vc4[j] = *reinterpret_cast<const u32x4 *>(p + (r * (D / 2) + d4_blk * 16));
+            vs4[j] = q[r * (D / 32) + d4_blk];
+        }
+    };
+    if constexpr (Q4) {
+        if (n4 > 0) {
+            load_k4(0);
+            load_v4(0);
+        }
+    }
+    // the first tree sub-tile of a wave with cache sub-tiles: its V only where that does not take the room that theirs go through
+    if (n > n4) {
+        issue_mask(n4);
+        issue(n4, true);
+        if (NS > 1 || n4 == 0) issue(n4, false);
+    }
+    if (NS > 1 && n4 == 0 && n > 1) {
         issue_mask(1);
         issue(1, true);
         issue(1, false);
@@ -159,7 +204,13 @@ __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveI
                             (D == 128 ? l32 * 256 + ((half ^ (l32 & 15)) << 4) : l32 * 128 + ((half ^ ((l32 >> 1) & 7)) << 4));
     const int lm = lane & 15, dim16 = (lane >> 4) & 1, vrow = 4 * half + (lm >> 2);
     const uint32_t v_base = lds_base + wave * S::ring_bytes + S::tile_bytes + vrow * S::row_bytes +
-                            ((D == 128 ? vrow & 3 : (vrow >> 1) & 1) << 6) + 32 * dim16 + 8 * (lm & 3);
+                            ((D == 128 ? vrow & 3 : (vrow >> 1) & 1) << 6) +
+                            (!Q4 ? 32 * dim16 + 8 * (lm & 3)
+                                 : (((2 * dim16 + ((lm & 3) >> 1)) ^ (D == 128 ? vrow & 3 : (vrow >> 1) & 3)) << 4) + 8 * (lm & 1));
+    // Q4: where a lane writes its block of V, in the stage that the second tree sub-tile will take (D = 128: the only one)
+    const uint32_t v4_stage = (uint32_t)((n4 + 1) % NS) * S::stage_bytes;
+    const uint32_t v4_out = lds_base + wave * S::ring_bytes + v4_stage + S::tile_bytes + d4_row * S::row_bytes +
+                            ((d4_blk ^ (D == 128 ? d4_row & 3 : (d4_row >> 1) & 1)) << 6) + ((D == 128 ? d4_row & 3 : (d4_row >> 1) & 3) << 4);
 
     const uint32_t m_base = lds_base + wave * S::ring_bytes + 2 * S::tile_bytes + l32 * 4;
 
@@ -318,7 +369,83 @@ __device__ __forceinline__ void attn_wave_rows(const Args &args, const AttnWaveI
         }
         if constexpr (RB == 2) static_for<0, 2 * DB>([&](auto I) { mfma_o(1, I); });
     };
-    for (int i = 0; i < n; ++i) step(i);
+    if constexpr (Q4) {
+        for (int i = 0; i < n4; ++i) {
+            // K: operands of the k-steps, and the next sub-tile's codes
+            uint32_t code[KS];
+#pragma unroll
+            for (int j = 0; j < KS / 2; ++j) {
+                const auto sw = __builtin_amdgcn_permlane32_swap(kc4[j / 2][2 * (j & 1)], kc4[j / 2][2 * (j & 1) + 1], false, false);
+                code[j] = sw[0], code[KS / 2 + j] = sw[1];
+            }
+            const uint32_t scales = ks4;
+            if (i + 1 < n4) load_k4(i + 1);
+            static_for<0, KS>([&](auto I) {
+                constexpr int ks = decltype(I)::value, b = ks / 2;
+                const float scale = __uint_as_float((scales >> (8 * b) << 23) & 0x7F800000u);
+                uint32_t w[4];
+                q4_decode8(code[ks], scale, w);
+                kf[ks] = (u32x4){w[0], w[1], w[2], w[3]};
+            });
+            const int valid = min(kSK, L - (t_first + i * NW) * kSK);
+            const uint32_t vbits = valid < kSK ? (1u << valid) - 1u : ~0u;
+            static_for<0, KS>([&](auto I) { mfma_s(0, I); });
+            // V, under the matrix instructions
+#pragma unroll
+            for (int j = 0; j < CW; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[4];
+                    q4_decode8(vc4[j][c], __uint_as_float(vs4[j] << 23), w);
+                    const u32x4 x = (u32x4){w[0], w[1], w[2], w[3]};
+                    if (j == 0) asm volatile("ds_write_b128 %0, %1" ::"v"(v4_out ^ (uint32_t)(c << 4)), "v"(x) : "memory");
+                    else asm volatile("ds_write_b128 %0, %1 offset:%2" ::"v"(v4_out ^ (uint32_t)(c << 4)), "v"(x), "n"(16 * S::row_bytes) : "memory");
+                }
+            if (i + 1 < n4) load_v4(i + 1);
+            // (LDS operations of a wave are executed in order: the reads find what was just written)
+            static_for<0, 2 * DB>([&](auto I) {
+                constexpr int t2 = decltype(I)::value / DB, db = decltype(I)::value % DB;
+                lds_rdtr<t2 * 16 * S::row_bytes>(vf[t2][db][0], (v_base + v4_stage) ^ (uint32_t)(db * 64));
+                lds_rdtr<(t2 * 16 + 8) * S::row_bytes>(vf[t2][db][1], (v_base + v4_stage) ^ (uint32_t)(db * 64));
+            });
+            prepare(0, valid < kSK, vbits);
+            if constexpr (RB == 2) {
+                static_for<0, 8>([&](auto I) {
+                    if constexpr (decltype(I)::value % 2 == 0) mfma_s(1, IC<decltype(I)::value / 2>{});
+                    weights(0, I);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            } else {
+                static_for<0, 8>([&](auto I) { weights(0, I); });
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int b = 0; b < DB; ++b) asm volatile("" : "+v"(vf[a][b][0]), "+v"(vf[a][b][1]));
+            if constexpr (RB == 2) {
+                prepare(1, valid < kSK, vbits);
+                static_for<0, 8>([&](auto I) {
+                    if constexpr (decltype(I)::value % 2 == 0) mfma_o(0, IC<decltype(I)::value / 2>{});
+                    weights(1, I);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                static_for<0, 2 * DB>([&](auto I) { mfma_o(1, I); });
+            } else {
+                static_for<0, 2 * DB>([&](auto I) { mfma_o(0, I); });
+            }
+        }
+        // the room that V went through is free: its reads have returned
+        if (n4 > 0) {
+            if (NS == 1 && n > n4) issue(n4, false);
+            if (NS > 1 && n > n4 + 1) {
+                issue_mask(n4 + 1);
+                issue(n4 + 1, true);
+                issue(n4 + 1, false);
+            }
+        }
+    }
+    for (int i = n4; i < n; ++i) step(i);
 
     // ---- the eight waves' results are combined in LDS (the rings are idle: every request of a wave
     //      has landed before its last sub-tile was worked on) ----

@@ -96,3 +96,21 @@ def test_reference_of_the_format():
         if np.abs(v).max() >= 4.0:
             again, s = q4_ref.encode(v)
             assert np.array_equal(again, code) and s[0, 0] == 127
+
+
+def test_attention_refuses_bad_arguments(lib, p):
+    off4, off1 = ctypes.c_void_p(p.value + 4), ctypes.c_void_p(p.value + 1)
+    good = dict(q=p, kc=p, ks=p, vc=p, vs=p, rows=8, kt=p, vt=p, mask=p, start=_i32(3), len=_i32(5), batch=1, T=5, Hq=4, Hkv=2, D=64,
+                scale=0.125, dtype=1, out=p)
+    bad = [dict(q=None), dict(kt=None), dict(vt=None), dict(mask=None), dict(out=None), dict(start=None), dict(len=None), dict(kc=None),
+           dict(ks=None), dict(vc=None), dict(vs=None), dict(kc=off4), dict(vs=off1), dict(q=off4), dict(out=off4), dict(mask=off4),
+           dict(batch=0), dict(batch=65), dict(T=0), dict(T=1026), dict(Hq=3), dict(Hkv=0), dict(D=40), dict(D=288), dict(D=16),
+           dict(scale=0.0), dict(scale=float("nan")), dict(dtype=2), dict(rows=7), dict(rows=0), dict(start=_i32(-1)), dict(len=_i32(-1)),
+           dict(start=_i32(4)), dict(start=_i32(0x7FFFFFFF))]
+    for change in bad:
+        a = dict(good, **change)
+        rc = lib.ddtree_verify_attn_q4(a["q"], a["kc"], a["ks"], a["vc"], a["vs"], a["rows"], a["kt"], a["vt"], a["mask"], a["start"],
+                                       a["len"], a["batch"], a["T"], a["Hq"], a["Hkv"], a["D"], a["scale"], a["dtype"], a["out"], None, 0, None)
+        assert rc == ERR_ARG, change
+    # a long key range that few workgroups share wants its scratch, as over a bf16 cache
+    assert lib.ddtree_verify_attn_q4(p, p, p, p, p, 8192, p, p, p, _i32(0), _i32(8192), 1, 257, 32, 8, 128, 0.088, 0, p, None, 0, None) == -2
