@@ -23,7 +23,7 @@
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls only enqueue
  *     kernels on it (no allocation, no memset or copy, no synchronisation); consecutive calls
  *     on one stream are ordered.  A caller may therefore record them into a HIP graph; the
- *     [host] arrays of a call (kv_offset, kv_start, kv_len, dst_row) travel as kernel arguments
+ *     [host] arrays of a call (kv_offset, kv_start, kv_len, dst_row, sampling options) travel as kernel arguments
  *     and are fixed in a recorded graph.
  *   - `workspace` [device] is scratch of at least ddtree_workspace_bytes(...) bytes, 256-byte
  *     aligned, whose contents need not survive between calls.  Calls on different streams need
@@ -233,6 +233,37 @@ int ddtree_accept_sampled(const float *target_logits, int batch, int T, int V,
                           const int32_t *n_nodes, float temperature, uint64_t seed, int32_t *path,
                           int32_t *n_accepted, int32_t *bonus_token, int32_t *posterior, int B,
                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One token per row by each sequence's own options, from given uniforms.  For a row of logits x with the largest M:
+ *     w_v = exp(-(M - x_v) / temperature), taken as 0 where (M - x_v) / temperature > 40 ln 2.
+ * In the order of falling logits, equal ones by ascending id, a token stays if
+ *     top_k    its rank is below top_k                                              (0: no such limit)
+ *     top_p    the sum of w in front of it is below top_p times the sum of all w, both over what top_k keeps   (1: off)
+ *     min_p    w_v >= min_p                                                         (0: off)
+ * so the likeliest token always stays.  The token is the first that stays, by ascending id, whose running sum of w (its own
+ * included) exceeds u times the sum of all that stay.  temperature = 0: the likeliest token, of equal ones the lowest id.
+ * Logits of -inf are never selected (nor NaN); a row of nothing else gives -1.  Weights and sums are taken in fp64: a
+ * token differs from this definition's only where u lies within about 1e-12 of a border.
+ *   logits      [device] fp32 [batch, T, V], V <= 2^22
+ *   temperature, top_k, top_p, min_p   [host] fp32 / int32 / fp32 / fp32 [batch]; temperature >= 0 and at most 1e30, top_k >= 0,
+ *               0 < top_p <= 1, 0 <= min_p <= 1 (DDTREE_ERR_ARG otherwise); the last three nullable (off)
+ *   uniforms    [device] fp32 [batch, T] in [0, 1) (what is outside counts as the end that it is past)
+ *   tokens      [device] int32 [batch, T]
+ * Workspace as ddtree_workspace_bytes says for N = max(1, T - 1).  T = 1: the next token of plain decoding.
+ */
+int ddtree_sample(const float *logits, int batch, int T, int V, const float *temperature,
+                  const int32_t *top_k, const float *top_p, const float *min_p, const float *uniforms,
+                  int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The verifier's walk with the target's tokens selected that way: ddtree_accept with ddtree_sample's selection at
+ * every node (rows past n_nodes are not read), which posterior receives. */
+int ddtree_accept_filtered(const float *target_logits, int batch, int T, int V, const int32_t *tokens,
+                           const int32_t *parent, const int32_t *depth, const int32_t *n_nodes,
+                           const float *temperature, const int32_t *top_k, const float *top_p,
+                           const float *min_p, const float *uniforms, int32_t *path, int32_t *n_accepted,
+                           int32_t *bonus_token, int32_t *posterior, int B, void *workspace,
+                           size_t workspace_bytes, void *stream);
 
 /*
  * Cache compaction (Section 4.4, last sentence): the cache keeps only the accepted path.  For

@@ -37,6 +37,9 @@ _SIGNATURES = {
     "ddtree_q4_store": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "ddtree_q4_append": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp]),
     "ddtree_q4_load": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]),
+    "ddtree_sample": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "ddtree_accept_filtered": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz,
+                                    _vp]),
     "ddtree_verify_attn_q4": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i,
                                    ctypes.c_float, _i, _vp, _vp, _sz, _vp]),
     "ddtree_set_build_algorithm": (_i, [_i]),
@@ -310,6 +313,63 @@ def compact(k_tree, v_tree, path, n_accepted, dst_row, batch, T, B, Hkv, D, k_ca
     _check(load().ddtree_compact(_ptr(k_tree), _ptr(v_tree), _ptr(path), _ptr(n_accepted), dst_p, batch, T, B,
                                  Hkv, D, k_tree.element_size(), _ptr(k_cache), _ptr(v_cache), _stream()),
            "ddtree_compact")
+
+
+def _options(batch, temperature, top_k, top_p, min_p):
+    """Sampling options as host arrays of batch entries (a scalar stands for all sequences) and their addresses."""
+    def one(v, dtype, what):
+        if not (type(v) is np.ndarray and v.dtype == dtype and v.flags.c_contiguous):
+            v = np.asarray(v, dtype=dtype)
+            v = np.full(batch, v, dtype) if v.ndim == 0 else np.ascontiguousarray(v)
+        if v.shape != (batch,):
+            raise DDTreeError(f"{what}: expected a number, or one for each of the {batch} sequences")
+        return v
+    arrays = (one(temperature, np.float32, "temperature"), one(top_k, np.int32, "top_k"), one(top_p, np.float32, "top_p"),
+              one(min_p, np.float32, "min_p"))
+    return arrays, tuple(a.ctypes.data for a in arrays)
+
+
+def sample(logits, uniforms, ws, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, defer=False):
+    """One token per row: logits fp32 [batch, T, V] (or [batch, V]), uniforms fp32 of a number a row -> int32 tokens like uniforms.
+    Options: a number, or one for each sequence; temperature 0 is greedy, top_k 0, top_p 1 and min_p 0 are off."""
+    _dev(logits, torch.float32, "logits")
+    _dev(uniforms, torch.float32, "uniforms")
+    if logits.dim() not in (2, 3) or uniforms.numel() * logits.shape[-1] != logits.numel():
+        raise DDTreeError("logits must be [batch, T, V] or [batch, V], with one uniform a row")
+    batch, T, V = logits.shape if logits.dim() == 3 else (logits.shape[0], 1, logits.shape[1])
+    _current(logits.get_device())
+    if out is None:
+        out = torch.empty_like(uniforms, dtype=torch.int32)
+    arrays, ptrs = _options(batch, temperature, top_k, top_p, min_p)
+    p, n = _ws(ws)
+    args = (_ptr(logits), batch, T, V, *ptrs, _ptr(uniforms), _ptr(out), p, n, _stream())
+    run = _call("ddtree_sample", args, out, defer)
+    return _keepalive(run, arrays) if defer else run
+
+
+def accept_filtered(target_logits, tokens, parent, depth, n_nodes, B, uniforms, ws, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                    out=None, want_posterior=True, defer=False):
+    """accept() with the target's tokens selected as sample() does, one uniform fp32 [batch, T] a node."""
+    _dev(target_logits, torch.float32, "target_logits")
+    _dev(uniforms, torch.float32, "uniforms")
+    batch, T, V = target_logits.shape
+    if uniforms.numel() != batch * T:
+        raise DDTreeError("uniforms must be [batch, T]")
+    for name, t, count in (("tokens", tokens, batch * T), ("parent", parent, batch * T), ("depth", depth, batch * T), ("n_nodes", n_nodes, batch)):
+        _dev(t, torch.int32, name)
+        if t.numel() != count:
+            raise DDTreeError(f"{name}: expected {count} entries")
+    _current(target_logits.get_device())
+    if out is None:
+        n_accepted = torch.empty_like(n_nodes)
+        out = dict(path=n_nodes.new_empty((batch, B + 1)), n_accepted=n_accepted, bonus_token=torch.empty_like(n_accepted),
+                   posterior=torch.empty_like(tokens) if want_posterior else None)
+    arrays, ptrs = _options(batch, temperature, top_k, top_p, min_p)
+    p, n = _ws(ws)
+    args = (_ptr(target_logits), batch, T, V, _ptr(tokens), _ptr(parent), _ptr(depth), _ptr(n_nodes), *ptrs, _ptr(uniforms),
+            _ptr(out["path"]), _ptr(out["n_accepted"]), _ptr(out["bonus_token"]), _ptr(out.get("posterior")), B, p, n, _stream())
+    run = _call("ddtree_accept_filtered", args, out, defer)
+    return _keepalive(run, arrays) if defer else run
 
 
 def _current(device):

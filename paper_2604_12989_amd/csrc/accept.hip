@@ -44,21 +44,6 @@ size_t accept_scratch_upper(int batch, int T, int V)
     return align_up((size_t)std::min(rows + 3071, rows * std::max(1, V / 4096)) * 8, 256);
 }
 
-// A segment's best: the value's order-preserving key, and below it the complement of the token id, so that the larger
-// of two is the larger value or, of equal ones, the lower id.
-typedef unsigned long long ArgPart;
-constexpr ArgPart kNoPart = 0ull;  // (below everything)
-__device__ __forceinline__ ArgPart arg_part(float v, int i) { return (ArgPart)float_key(v) << 32 | (uint32_t)~i; }
-__device__ __forceinline__ int arg_token(ArgPart p) { return (int)~(uint32_t)p; }
-// Against the lane that CTRL names.  (On two registers through DPP a step costs some 50 cycles, value and id exchanged
-// through LDS 190: scan and walk, launch to launch, of 17 rows of 151936 8.1 -> 6.8 us, 65 of 32003 7.7 -> 6.5, 257 of 151936 28.2 -> 27.6.)
-template <int CTRL, int ROW_MASK = 0xF>
-__device__ __forceinline__ ArgPart arg_max_dpp(ArgPart p)
-{
-    const ArgPart o = (ArgPart)dpp_u<CTRL, ROW_MASK>((uint32_t)(p >> 32)) << 32 | dpp_u<CTRL, ROW_MASK>((uint32_t)p);
-    return o > p ? o : p;
-}
-
 __device__ __forceinline__ void arg_update(float &bv, int &bi, float v, int i)
 {
     if (v > bv || (v == bv && i < bi)) {
@@ -106,13 +91,7 @@ __device__ __forceinline__ float sample_key(float logit, uint32_t h, const Sampl
 // The workgroup's best, valid in thread 0.
 __device__ __forceinline__ ArgPart workgroup_best(float bv, int bi, ArgPart *s_best)
 {
-    ArgPart p = arg_part(bv, bi);
-    p = arg_max_dpp<0xB1>(p);
-    p = arg_max_dpp<0x4E>(p);
-    p = arg_max_dpp<0x141>(p);
-    p = arg_max_dpp<0x140>(p);
-    p = arg_max_dpp<0x142, 0xA>(p);
-    p = arg_max_dpp<0x143, 0xC>(p);
+    ArgPart p = wave_arg_max(arg_part(bv, bi));
     if ((threadIdx.x & 63) == 63) s_best[threadIdx.x >> 6] = p;
     __syncthreads();
     p = s_best[0];
@@ -370,6 +349,19 @@ __global__ __launch_bounds__(kWalkMaxThreads) void accept_walk_kernel(
     }
 }
 
+// The walk over what `splits` partial results a row select.
+void accept_walk_launch(const ArgPart *part, int batch, int T, int splits, int B, const int32_t *tokens, const int32_t *parent,
+                        const int32_t *depth, const int32_t *n_nodes, int32_t *path, int32_t *n_accepted, int32_t *bonus_token,
+                        int32_t *posterior, hipStream_t st)
+{
+    // as many lanes per row as there are partial results, within one workgroup; every row at once (T = 1025: but one)
+    int lanes = 1;
+    while (lanes < 64 && lanes < splits && 2 * lanes * T <= kWalkMaxThreads) lanes *= 2;
+    const int threads = std::min(kWalkMaxThreads, std::max(64, (lanes * T + 63) / 64 * 64));
+    DDT_LAUNCH(DDTREE_KERNEL_ACCEPT_WALK, st, accept_walk_kernel, dim3(batch), dim3(threads), 0, st, part, T, splits, lanes,
+                       B, tokens, parent, depth, n_nodes, path, n_accepted, bonus_token, posterior);
+}
+
 struct CompactArgs {
     int32_t dst_row[DDTREE_MAX_BATCH];
 };
@@ -446,12 +438,7 @@ static int accept_impl(const float *target_logits, int batch, int T, int V, cons
     else
         DDT_LAUNCH(DDTREE_KERNEL_ACCEPT_ARGMAX, st, accept_argmax_kernel, dim3(p.splits, T, batch), dim3(kArgmaxThreads), 0, st,
                    target_logits, T, V, p.seg_len, p.splits, n_nodes, part);
-    // as many lanes per row as there are partial results, within one workgroup; every row at once (T = 1025: but one)
-    int lanes = 1;
-    while (lanes < 64 && lanes < p.splits && 2 * lanes * T <= kWalkMaxThreads) lanes *= 2;
-    const int threads = std::min(kWalkMaxThreads, std::max(64, (lanes * T + 63) / 64 * 64));
-    DDT_LAUNCH(DDTREE_KERNEL_ACCEPT_WALK, st, accept_walk_kernel, dim3(batch), dim3(threads), 0, st, part, T, p.splits, lanes,
-                       B, tokens, parent, depth, n_nodes, path, n_accepted, bonus_token, posterior);
+    accept_walk_launch(part, batch, T, p.splits, B, tokens, parent, depth, n_nodes, path, n_accepted, bonus_token, posterior, st);
     return launch_status();
 }
 

@@ -59,6 +59,8 @@ extern "C" size_t ddtree_workspace_bytes(int batch, int B, int V, int N, int Hq,
     if (a > need) need = a;
     const size_t c = accept_scratch_upper(batch, T, V);
     if (c > need) need = c;
+    const size_t f = sample_scratch_upper(batch, T, V);
+    if (f > need) need = f;
     return need < 256 ? 256 : need;
 }
 
@@ -178,5 +180,5 @@ extern "C" int ddtree_selftest_host(void)
                     for (int t = T; t >= 2; t -= 1 + t / 5)
                         if (accept_plan(b, t, V).bytes > accept_scratch_upper(batch, T, V)) return 10024;
             }
-    return 0;
+    return sample_selftest_host();
 }
