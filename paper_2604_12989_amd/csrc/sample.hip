@@ -13,10 +13,12 @@
 //          of its weights (where the row's sum is asked for) relative to its own best, and a list of its largest
 //          elements with the bound that they reach.
 //   pick   one workgroup per row.  Without filters: the segment where the running sum passes u S, then the token in it,
-//          from one more read of the segment.  With filters: what stays is nearly always among the listed elements
-//          above the largest of the segments' bounds (about 1200 of a row): their ranks and the weights in front of them
-//          from buckets.  Otherwise (flat rows, ties in thousands) the row is read again, three or four times: thresholds
-//          by buckets over the logits, the sums of chunks, the token.
+//          from one more read of the segment.  With filters: what stays is mostly among the listed elements above the
+//          largest of the segments' bounds (about 1200 of a row): their ranks and the weights in front of them from
+//          buckets.  A row of which that does not hold (thousands of tokens stay) is put on a list.
+//   again  what is on the list, many workgroups a row: each leaves, for 4096 elements, the count and the weight in front
+//          of each of 256 steps of the logit; the last one to come adds them up, reads the row once more for the elements
+//          of the one step where the border lies, and draws the token.
 // Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 62 bits allow):
 // their order does not matter.
 #include <algorithm>
@@ -26,7 +28,12 @@
 namespace ddt {
 
 constexpr int kScanThreads = 256;
-constexpr int kPickThreads = 512;
+constexpr int kPickThreads = 256;
+constexpr int kAgainThreads = 512;
+constexpr int kAgainGrid = 512;     // workgroups that look for rows on the list
+constexpr int kPart = 8192;         // elements of a row that a workgroup takes at a time there
+constexpr int kSteps = 256;         // steps of the logit
+constexpr int kSlots = 256;         // rows on the list that many workgroups take
 constexpr int kCandidates = 2048;   // listed elements that one row's pick holds
 constexpr int kCandBuckets = 1024;
 constexpr int kHistBuckets = 2048;
@@ -52,12 +59,23 @@ struct SegStat {
 static_assert(sizeof(SegStat) == 32, "one line of two 16-byte stores");
 
 struct SamplePlan {
-    int segs, seg_len, vecs, hot_rank, hot_cap;
-    size_t stat_off, hot_off, part_off, bytes;
+    int segs, seg_len, vecs, hot, hot_cap;  // elements that a list is to hold, and room for
+    int parts, slots;  // of a row on the list; rows that the steps' sums have room for
+    size_t stat_off, hot_off, part_off, hard_off, step_off, bytes;
+};
+
+// A row on the list, and what is known of it.
+struct HardRow {
+    double sum, best;   // of its weights (0: not known), its largest logit
+    int32_t row, arrived;
+};
+// In front of each step of the logit, over kPart elements: their weights and their number.
+struct StepSum {
+    ArgPart mass, count;
 };
 
 // Segments of 6140 elements, 24 a thread with room for a row that starts inside a 16-byte group; of 2044 where those make
-// fewer than two workgroups a compute unit.  The lists together hold about 1600 of a row's largest, enough for the usual top-k.
+// fewer than two workgroups a compute unit.  The lists together hold about 1400 of a row's largest, enough for the usual top-k.
 static SamplePlan sample_plan(int batch, int T, int V)
 {
     SamplePlan p{};
@@ -65,14 +83,18 @@ static SamplePlan sample_plan(int batch, int T, int V)
     p.vecs = rows * ((V + 6139) / 6140) < 512 && V <= 2044ll * kMaxSegs ? 2 : 6;
     p.seg_len = p.vecs * 1024 - 4;
     p.segs = (V + p.seg_len - 1) / p.seg_len;
-    p.hot_rank = std::min(200, std::max(16, 1600 / p.segs));
+    p.hot = std::min(200, std::max(16, 1400 / p.segs));
     p.hot_cap = 64;
-    while (p.hot_cap < 2 * p.hot_rank) p.hot_cap *= 2;
+    while (p.hot_cap < 2 * p.hot) p.hot_cap *= 2;
     const size_t per = (size_t)rows * p.segs;
     p.stat_off = 0;
     p.hot_off = align_up(per * sizeof(SegStat), 256);
     p.part_off = p.hot_off + align_up(per * p.hot_cap * 8, 256);
-    p.bytes = p.part_off + align_up((size_t)rows * 8, 256);
+    p.parts = (V + kPart - 1) / kPart;
+    p.hard_off = p.part_off + align_up((size_t)rows * 8, 256);
+    p.step_off = p.hard_off + align_up(256 + (size_t)rows * sizeof(HardRow), 256);
+    p.slots = (int)std::min<long long>(rows, kSlots);
+    p.bytes = p.step_off + align_up((size_t)p.slots * p.parts * ((kSteps + 1) * sizeof(StepSum)), 256);
     return p;
 }
 
@@ -82,11 +104,12 @@ size_t sample_scratch_upper(int batch, int T, int V)
     const size_t rows = (size_t)batch * T;
     size_t most = 0;
     if (V > kSampleMaxV) V = kSampleMaxV;
-    // (a segment's list is at most four times what 1600 divided by the segments asks for, or 64; short segments only below 512
+    // (a segment's list is at most four times what 1400 divided by the segments asks for, or 64; short segments only below 512
     // workgroups of long ones)
     const size_t long_segs = rows * ((V + 6139) / 6140), short_segs = std::min<size_t>(rows * ((V + 2043) / 2044), 512 * 4 + rows);
     const size_t segs = std::max(long_segs, short_segs);
-    most = segs * (sizeof(SegStat) + 64 * 8) + rows * (size_t)(4 * 1600) * 8 + rows * 8 + 1024;
+    most = segs * (sizeof(SegStat) + 64 * 8) + rows * (size_t)(4 * 1600) * 8 + rows * (8 + sizeof(HardRow)) + 2048 +
+           std::min<size_t>(rows, kSlots) * ((V + kPart - 1) / kPart) * ((kSteps + 1) * sizeof(StepSum));
     return align_up(most, 256);
 }
 
@@ -112,9 +135,10 @@ __device__ __forceinline__ double exp2_of(double t)
 // What counts as a logit: NaN as -inf (never selected), +inf as the largest finite number.
 __device__ __forceinline__ float clean(float x)
 {
-    const uint32_t b = __float_as_uint(x);
-    if ((b & 0x7FFFFFFFu) > 0x7F800000u) return -INFINITY;
-    return b == 0x7F800000u ? 3.4028235e38f : x;
+    // (the median of three is the smaller of the other two where one is no number; in the compiler's own terms there are none)
+    float y;
+    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "v"(-INFINITY), "v"(3.4028235e38f));
+    return y;
 }
 constexpr uint32_t kKeyOfNone = 0x007FFFFFu;  // float_key(-inf)
 
@@ -138,8 +162,9 @@ __device__ __forceinline__ int behind_boundary(const float *p) { return (int)((r
 
 template <int VECS>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
-    const float *__restrict__ logits, int T, int V, int seg_len, int segs, int hot_rank, int hot_cap,
-    const int32_t *__restrict__ n_nodes, SegStat *__restrict__ stat, ArgPart *__restrict__ hot, SampleOpts opt)
+    const float *__restrict__ logits, int T, int V, int seg_len, int segs, int hot_size, int hot_cap,
+    const int32_t *__restrict__ n_nodes, SegStat *__restrict__ stat, ArgPart *__restrict__ hot, uint32_t *__restrict__ n_hard,
+    SampleOpts opt)
 {
     __shared__ ArgPart s_best[kScanThreads / 64];
     __shared__ double s_sum[kScanThreads / 64];
@@ -149,6 +174,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
     __shared__ uint32_t s_bound;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int seg = blockIdx.x, i = blockIdx.y, seq = blockIdx.z;
+    if (tid == 0 && (seg | i | seq) == 0) *n_hard = 0u;
     if (n_nodes && i > n_nodes[seq]) return;  // padding row
     const size_t row = (size_t)seq * T + i;
     const int start = seg * seg_len, n = min(seg_len, V - start);
@@ -206,9 +232,14 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
         if (lane == 63) s_sum[wave] = sum, s_low[wave] = low;
     }
     if (filtered && tau > 0.0f && wave == 0) {
-        // A bound that about hot_rank of the thread maxima reach, by bisection over their keys
+        // A bound that about `size` elements reach, by bisection over the keys of the thread maxima: as many as
+        // 256 (1 - e^(-size / 256)) of these reach a bound that `size` elements at random places do.  Of top-k's tokens a
+        // segment has its share and some more; too few listed (rows that are not at random) go on the list of rows.
         uint32_t k[4], lo = kKeyOfNone + 1u;
         if (n_alive > hot_cap) {
+            const int top_k = opt.top_k[seq];
+            const int size = top_k > 0 ? min(hot_size, 3 * top_k / segs + 16) : hot_size;
+            const int rank = max(1, (int)(256.0f - 256.0f * __builtin_amdgcn_exp2f((float)size * (-1.44269504f / 256.0f))));
 #pragma unroll
             for (int u = 0; u < 4; ++u) k[u] = float_key(s_max[u * 64 + lane]);
             auto reach = [&](uint32_t b) {
@@ -217,14 +248,15 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
                 for (int u = 0; u < 4; ++u) c += __popcll(__builtin_amdgcn_ballot_w64(k[u] >= b));
                 return c;
             };
+            lo = max(lo, wave_min_u32(min(min(k[0], k[1]), min(k[2], k[3]))));
             uint32_t hi = (uint32_t)(best >> 32) + 1u;
-            if (reach(lo) > hot_rank) {
+            if (reach(lo) > rank) {
                 while (hi - lo > 1u) {
                     const uint32_t mid = lo + (hi - lo) / 2u;
                     const int c = reach(mid);
-                    if (c >= hot_rank) lo = mid;
+                    if (c >= rank) lo = mid;
                     else hi = mid;
-                    if (c >= hot_rank && c <= hot_rank + hot_rank / 8) break;
+                    if (c >= rank && c <= rank + rank / 8) break;
                 }
             }
         } else {
@@ -234,19 +266,27 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
     }
     __syncthreads();
     if (filtered && tau > 0.0f) {
-        const uint32_t bound = s_bound;
-        const uint32_t at_least = max(bound, kKeyOfNone + 1u);
+        const float least = key_float(max(s_bound, kKeyOfNone + 1u));
         ArgPart *const list = hot + (row * segs + seg) * (size_t)hot_cap;
-        if (float_key(bv) >= at_least) {
+        // (the wave's share of the list is taken at once: an LDS atomic for each element costs the scan 8 us)
+        int listed = 0;
 #pragma unroll
-            for (int j = 0; j < VECS; ++j)
+        for (int j = 0; j < VECS; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (float_key(x[j][e]) >= at_least) {
-                        const int at = atomicAdd(&s_listed, 1);
-                        if (at < hot_cap) list[at] = arg_part(x[j][e], start + 4 * (j * kScanThreads + tid) - a + e);
-                    }
-        }
+            for (int e = 0; e < 4; ++e) listed += __popcll(__builtin_amdgcn_ballot_w64(x[j][e] >= least));
+        int at = 0;
+        if (lane == 0 && listed > 0) at = atomicAdd(&s_listed, listed);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned long long who = __builtin_amdgcn_ballot_w64(x[j][e] >= least);
+                if (who == 0ull) continue;
+                const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+                if (x[j][e] >= least && mine < hot_cap) list[mine] = arg_part(x[j][e], start + 4 * (j * kScanThreads + tid) - a + e);
+                at += __popcll(who);
+            }
         __syncthreads();
     }
     if (tid == 0) {
@@ -263,63 +303,46 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
     }
 }
 
-// ---- pick: what a workgroup shares ----
-struct PickShared {
-    union {
-        struct {
-            uint32_t key[kCandidates], id[kCandidates];
-            ArgPart w[kCandidates];
-            uint16_t order[kCandidates];
-            ArgPart mass[kCandBuckets];
-            uint32_t count[kCandBuckets], cursor[kCandBuckets];
-        } c;
-        struct {
-            ArgPart mass[kHistBuckets];
-            uint32_t count[kHistBuckets];
-            ArgPart list[kCandidates], w[kCandidates];
-        } h;
-        double chunk[kMaxChunks + kPickThreads];
-        double seg[kMaxSegs];
-    };
-    double wave_d[kPickThreads / 64];
-    ArgPart wave_u[kPickThreads / 64];
-    ArgPart found, base;
-    double found_d;
-    int n, last, token;
-};
-
-template <class X>
-__device__ __forceinline__ X shfl_up(X v, int d)
+// ---- what pick and again share ----
+template <int CTRL, int ROW_MASK, class X>
+__device__ __forceinline__ X dpp64_or_zero(X v)
 {
     static_assert(sizeof(X) == 8, "64 bits");
     const ArgPart u = __builtin_bit_cast(ArgPart, v);
-    const uint32_t lo = __shfl_up((uint32_t)u, d, 64), hi = __shfl_up((uint32_t)(u >> 32), d, 64);
-    return __builtin_bit_cast(X, (ArgPart)hi << 32 | lo);
+    return __builtin_bit_cast(X, (ArgPart)(uint32_t)dpp_or_zero<CTRL, ROW_MASK>((int)(u >> 32)) << 32 |
+                                     (uint32_t)dpp_or_zero<CTRL, ROW_MASK>((int)(uint32_t)u));
 }
-// Sum over the threads in front of this one, and over all (both in one fixed order).
+// Inclusive sum over the wave's lanes (see wave_scan_inclusive_i32).
 template <class X>
+__device__ __forceinline__ X wave_scan64(X v)
+{
+    v += dpp64_or_zero<0x111, 0xF>(v);
+    v += dpp64_or_zero<0x112, 0xF>(v);
+    v += dpp64_or_zero<0x114, 0xF>(v);
+    v += dpp64_or_zero<0x118, 0xF>(v);
+    v += dpp64_or_zero<0x142, 0xA>(v);
+    v += dpp64_or_zero<0x143, 0xC>(v);
+    return v;
+}
+// Sum over the threads in front of this one, and over all (both in one fixed order).  waves: one entry a wave.
+template <int NT, class X>
 __device__ __forceinline__ X block_scan(X v, X *waves, X &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    X s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const X o = shfl_up(s, d);
-        s = lane >= d ? s + o : s;
-    }
+    const X s = wave_scan64(v);
+    // (the neighbour's: the inclusive sum less the own value, without a subtraction)
+    X up = dpp64_or_zero<0x138, 0xF>(s);  // wave_shr:1
     __syncthreads();
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     X before = X(0);
     total = X(0);
 #pragma unroll
-    for (int w = 0; w < kPickThreads / 64; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         before = w < wave ? before + waves[w] : before;
         total += waves[w];
     }
-    // (the inclusive sum less the own value, taken from the neighbour so that nothing is subtracted)
-    const X up = shfl_up(s, 1);
-    return before + (lane > 0 ? up : X(0));
+    return before + up;
 }
 
 // A row, and what stays of it as far as that is known.
@@ -338,34 +361,91 @@ struct PickRow {
         const double w = exp2_of(t);
         return w >= min_w ? w : 0.0;
     }
-    template <class F>
+    template <int NT, class F>
     __device__ __forceinline__ void each(F &&f) const
     {
+        constexpr int kAhead = 4;
         const int groups = (V + a + 3) >> 2;
-        for (int g = threadIdx.x; g < groups; g += 2 * kPickThreads) {
-            const float4 p = load_group(x, g, a, V), q = load_group(x, g + kPickThreads, a, V);
-            const float e[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+        for (int g = threadIdx.x; g < groups; g += kAhead * NT) {
+            float4 p[kAhead];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (e[u] > -INFINITY) f(e[u], 4 * (g + (u >> 2) * kPickThreads) - a + (u & 3));
+            for (int u = 0; u < kAhead; ++u) p[u] = load_group(x, g + u * NT, a, V);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const float e[4] = {p[u].x, p[u].y, p[u].z, p[u].w};
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (e[v] > -INFINITY) f(e[v], 4 * (g + u * NT) - a + v);
+            }
         }
     }
 };
+__device__ __forceinline__ PickRow pick_row(const float *logits, size_t row, int V, double M, float tau)
+{
+    PickRow r;
+    r.x = logits + row * (size_t)V;
+    r.V = V;
+    r.a = behind_boundary(r.x);
+    r.M = M;
+    r.c = 1.4426950408889634 / (double)tau;
+    r.floor = 0ull;
+    r.min_w = 0.0;
+    return r;
+}
+// Four elements at p, of which n > 0 are there.  (Rows of any length: 4-byte alignment.)
+__device__ __forceinline__ float4 load_four(const float *p, int n)
+{
+    typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+    float4 x = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (n >= 4) {
+        const four f = *reinterpret_cast<const four *>(p);
+        x = make_float4(clean(f.x), clean(f.y), clean(f.z), clean(f.w));
+    } else {
+        if (n > 0) x.x = clean(p[0]);
+        if (n > 1) x.y = clean(p[1]);
+        if (n > 2) x.z = clean(p[2]);
+    }
+    return x;
+}
+// u from [0, 1): what is below, or no number, counts as 0, what is above as the largest float below 1
+__device__ __forceinline__ float clean_uniform(float u)
+{
+    const uint32_t b = __float_as_uint(u);
+    return b > 0x7F800000u ? 0.0f : b >= 0x3F800000u ? 0x1.fffffep-1f : u;
+}
+__device__ __forceinline__ void put_token(int token, size_t row, ArgPart *part, int32_t *tokens)
+{
+    if (threadIdx.x != 0) return;
+    if (tokens) tokens[row] = token;
+    else part[row] = 1ull << 32 | (uint32_t)~token;
+}
 
+template <int NT>
+struct LocateShared {
+    double wave_d[NT / 64 < 2 ? 2 : NT / 64];
+    int last, token;
+};
 // The element of [start, start + n) where the running sum, `base` in front of it, exceeds `target` (the last one with a
 // weight, should rounding leave none).  c0, c1: the running sum in front of it and behind it.
-__device__ int pick_locate(const PickRow &r, int start, int n, double base, double target, PickShared &sh, double &c0, double &c1)
+template <int NT>
+__device__ int pick_locate(const PickRow &r, int start, int n, double base, double target, LocateShared<NT> &sh, double &c0, double &c1)
 {
-    const int per = (n + kPickThreads - 1) / kPickThreads, from = start + (int)threadIdx.x * per, to = min(from + per, start + n);
+    // (a multiple of four elements a thread: as many loads of 16 bytes where the row allows)
+    const int per = ((n + NT - 1) / NT + 3) / 4 * 4, from = start + (int)threadIdx.x * per, to = min(from + per, start + n);
     double mine = 0.0, total;
     int last = -1;
-    for (int e = from; e < to; ++e) {
-        const double w = r.weight(clean(r.x[e]), e);
-        if (w > 0.0) last = e;
-        mine += w;
+    for (int g = from; g < to; g += 4) {
+        const float4 p = load_four(r.x + g, to - g);
+        const float e[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const double w = e[u] > -INFINITY ? r.weight(e[u], g + u) : 0.0;
+            if (w > 0.0) last = g + u;
+            mine += w;
+        }
     }
     if (threadIdx.x == 0) sh.last = -1, sh.token = -1;
-    const double before = base + block_scan(mine, sh.wave_d, total);
+    const double before = base + block_scan<NT>(mine, sh.wave_d, total);
     if (last >= 0) atomicMax(&sh.last, last);
     if (last >= 0 && before <= target && target < before + mine) atomicMax(&sh.token, (int)threadIdx.x);
     __syncthreads();
@@ -393,11 +473,354 @@ __device__ int pick_locate(const PickRow &r, int start, int n, double base, doub
     return token;
 }
 
-// The composite of the last element, in falling order, with less than `limit` in front of it: elements counted, or their
-// weights summed (in units of 1 / unit).  Elements below r.floor do not take part; r.floor if all stay.
-template <bool MASS>
-__device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, PickShared &sh)
+struct PickShared {
+    union {
+        struct {
+            uint32_t key[kCandidates], id[kCandidates];
+            ArgPart w[kCandidates];
+            uint16_t order[kCandidates];
+            ArgPart mass[kCandBuckets];
+            uint32_t count[kCandBuckets], cursor[kCandBuckets];
+        } c;
+        double seg[kMaxSegs];
+    };
+    int32_t listed[kMaxSegs];
+    ArgPart wave_u[kPickThreads / 64];
+    LocateShared<kPickThreads> locate;
+    int n, last, token;
+};
+
+__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
+    const float *__restrict__ logits, int T, int V, int seg_len, int segs, int hot_cap,
+    const int32_t *__restrict__ n_nodes, const float *__restrict__ uniforms, const SegStat *__restrict__ stat_all,
+    const ArgPart *__restrict__ hot_all, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, uint32_t *__restrict__ n_hard,
+    HardRow *__restrict__ hard, SampleOpts opt)
 {
+    __shared__ PickShared sh;
+    const int tid = threadIdx.x, i = blockIdx.x, seq = blockIdx.y;
+    if (n_nodes && i > n_nodes[seq]) return;  // padding row
+    const size_t row = (size_t)seq * T + i;
+    const SegStat *const stat = stat_all + row * segs;
+    const ArgPart *const hot = hot_all + row * segs * (size_t)hot_cap;
+    const float tau = opt.tau[seq], top_p = opt.top_p[seq], min_p = opt.min_p[seq];
+    const int top_k = opt.top_k[seq];
+    const bool filtered = top_k > 0 || top_p < 1.0f || min_p > 0.0f;
+    const float u = clean_uniform(uniforms[row]);
+    // the lists are requested before anything is known of them (what is past a list's end is not looked at)
+    constexpr int kAhead = 8;
+    const int slots = filtered && tau > 0.0f ? segs * hot_cap / 2 : 0;  // pairs
+    ulonglong2 ahead[kAhead];
+#pragma unroll
+    for (int v = 0; v < kAhead; ++v)
+        if (tid + v * kPickThreads < slots) ahead[v] = reinterpret_cast<const ulonglong2 *>(hot)[tid + v * kPickThreads];
+
+    // the row's best, and the largest of the bounds (a list that is not complete: no bound holds)
+    ArgPart best = kNoPart;
+    uint32_t bound = 0u;
+    for (int s = tid; s < segs; s += kPickThreads) {
+        const ArgPart b = stat[s].best;
+        const int listed = stat[s].listed;
+        best = b > best ? b : best;
+        bound = max(bound, listed > hot_cap ? ~0u : stat[s].bound);
+        sh.listed[s] = listed;
+    }
+    best = wave_arg_max(best);
+    bound = ~wave_min_u32(~bound);
+    if ((tid & 63) == 63) sh.wave_u[tid >> 6] = best, sh.locate.wave_d[tid >> 6] = (double)bound;
+    __syncthreads();
+    best = kNoPart;
+#pragma unroll
+    for (int w = 0; w < kPickThreads / 64; ++w) {
+        best = sh.wave_u[w] > best ? sh.wave_u[w] : best;
+        bound = max(bound, (uint32_t)sh.locate.wave_d[w]);
+    }
+    __syncthreads();
+    if (best == kNoPart) return put_token(-1, row, part, tokens);
+    if (!(tau > 0.0f)) return put_token(arg_token(best), row, part, tokens);
+
+    const PickRow r = pick_row(logits, row, V, (double)key_float((uint32_t)(best >> 32)), tau);
+    const bool has_sum = top_k == 0 && (top_p < 1.0f || !filtered);
+    double Z = 0.0;
+    auto put_on_list = [&](double sum) {
+        if (tid == 0) hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, (int32_t)row, 0};
+    };
+
+    // The row's sum.  A segment has also counted elements that are too small beside the row's best but not beside its own:
+    // `slack` bounds what they add (each is below 2^-40, if there are any).  Where this could change a decision, the row goes
+    // on the list.
+    double slack = 0.0;
+    if (has_sum) {
+        const int per = (segs + kPickThreads - 1) / kPickThreads, from = tid * per, to = min(from + per, segs);
+        double mine = 0.0;
+        bool doubt = false;
+        for (int s = from; s < to; ++s) {
+            double w = 0.0;
+            const ArgPart b = stat[s].best;
+            if (b != kNoPart) {
+                const double t = r.log_weight(key_float((uint32_t)(b >> 32)));
+                if (t >= kCut) {
+                    w = exp2_of(t) * stat[s].sum;
+                    doubt = doubt || !(r.log_weight(stat[s].low) >= kCut);
+                }
+            }
+            if (!filtered) sh.seg[s] = w;
+            mine += w;
+        }
+        const double before = block_scan<kPickThreads>(mine, sh.locate.wave_d, Z);
+        if (__syncthreads_or(doubt ? 1 : 0)) slack = (double)V * 0x1p-40;
+        if (!filtered) {
+            const double target = (double)u * Z;
+            if (tid == 0) sh.n = -1;
+            __syncthreads();
+            double b = before;
+            for (int s = from; s < to; ++s) {
+                if (sh.seg[s] > 0.0 && b <= target) atomicMax(&sh.n, s);
+                const double w = sh.seg[s];
+                sh.seg[s] = b;
+                b += w;
+            }
+            __syncthreads();
+            const int s = sh.n;
+            const double base = sh.seg[s];
+            double c0, c1;
+            const int token = pick_locate<kPickThreads>(r, s * seg_len, min(seg_len, V - s * seg_len), base, target, sh.locate, c0, c1);
+            if (slack > 0.0 && !(c0 <= (double)u * (Z - slack) && target < c1 - slack)) return put_on_list(0.0);
+            return put_token(token, row, part, tokens);
+        }
+    }
+
+    // ---- the listed elements that reach the bound ----
+    auto &c = sh.c;
+    const uint32_t at_least = max(bound, kKeyOfNone + 1u);
+    if (tid == 0) sh.n = 0;
+    for (int b = tid; b < kCandBuckets; b += kPickThreads) c.mass[b] = 0ull, c.count[b] = 0u;
+    __syncthreads();
+    if (bound != ~0u) {
+        auto take = [&](ArgPart h) {
+            const int at = atomicAdd(&sh.n, 1);
+            if (at < kCandidates) c.key[at] = (uint32_t)(h >> 32), c.id[at] = (uint32_t)arg_token(h);
+        };
+        auto look = [&](int pair, const ulonglong2 &h) {
+            const int s = 2 * pair / hot_cap, left = sh.listed[s] - (2 * pair - s * hot_cap);
+            if (left > 0 && (uint32_t)(h.x >> 32) >= at_least) take(h.x);
+            if (left > 1 && (uint32_t)(h.y >> 32) >= at_least) take(h.y);
+        };
+#pragma unroll
+        for (int v = 0; v < kAhead; ++v)
+            if (tid + v * kPickThreads < slots) look(tid + v * kPickThreads, ahead[v]);
+        for (int k = tid + kAhead * kPickThreads; k < slots; k += kPickThreads) look(k, reinterpret_cast<const ulonglong2 *>(hot)[k]);
+    }
+    __syncthreads();
+    const int n = sh.n;
+    if (bound == ~0u || n > kCandidates) return put_on_list(slack > 0.0 ? 0.0 : Z);
+    // (below the bound nothing has a weight: the list is all there is)
+    const double t_bound = bound == 0u ? -1e30 : r.log_weight(key_float(bound));
+    const bool all = bound == 0u || t_bound < kCut;
+    // buckets in falling order: equal steps between the best and the least listed (for elements without a weight, the last)
+    const double span = fmax(all ? kCut : t_bound, kCut);
+    const double step = span < 0.0 ? (double)(kCandBuckets - 1) / span : 0.0;
+    auto bucket_of = [&](double t) { return min(kCandBuckets - 1, max(0, (int)(fmax(t, 2.0 * kCut) * step))); };
+    constexpr int kEach = kCandidates / kPickThreads;
+    uint16_t bucket[kEach];
+    bool counts[kEach];  // has a weight, and not below min-p
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) {
+        const int k = tid + v * kPickThreads;
+        bucket[v] = 0, counts[v] = false;
+        if (k >= n) continue;
+        const double t = r.log_weight(key_float(c.key[k])), weight = exp2_of(t);
+        const ArgPart w = t >= kCut ? (ArgPart)(weight * 0x1p52 + 0.5) : 0ull;
+        counts[v] = t >= kCut && weight >= (double)min_p;
+        c.w[k] = w;
+        bucket[v] = (uint16_t)bucket_of(t);
+        atomicAdd(&c.mass[bucket[v]], w);
+        atomicAdd(&c.count[bucket[v]], 1u);
+    }
+    __syncthreads();
+    constexpr int kPer = kCandBuckets / kPickThreads;
+    ArgPart m[kPer], q[kPer], m_mine = 0ull, q_mine = 0ull, m_all, q_all;
+#pragma unroll
+    for (int v = 0; v < kPer; ++v) {
+        m[v] = c.mass[tid * kPer + v], q[v] = c.count[tid * kPer + v];
+        m_mine += m[v], q_mine += q[v];
+    }
+    ArgPart m_front = block_scan<kPickThreads>(m_mine, sh.wave_u, m_all), q_front = block_scan<kPickThreads>(q_mine, sh.wave_u, q_all);
+#pragma unroll
+    for (int v = 0; v < kPer; ++v) {
+        c.mass[tid * kPer + v] = m_front, c.cursor[tid * kPer + v] = (uint32_t)q_front;
+        m_front += m[v], q_front += q[v];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kEach; ++v)
+        if (tid + v * kPickThreads < n) c.order[atomicAdd(&c.cursor[bucket[v]], 1u)] = (uint16_t)(tid + v * kPickThreads);
+    __syncthreads();
+    // rank and weight in front of each; where its bucket lies behind the end of top-k or top-p, or the element has no weight, it
+    // does not matter which (a row's list is mostly made of those: 50 of 1200 stay at top-k 50)
+    const double p_ends = top_k == 0 && top_p < 1.0f ? (double)top_p * Z * 0x1p52 : 0x1p64;
+    int rank[kEach];
+    ArgPart front[kEach], kept = 0ull, sum;
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) {
+        const int k = tid + v * kPickThreads;
+        rank[v] = 0, front[v] = 0ull;
+        if (k >= n) continue;
+        const int b = bucket[v], end = (int)c.cursor[b], begin = end - (int)c.count[b];
+        const uint32_t key = c.key[k], id = c.id[k];
+        ArgPart f = c.mass[b];
+        int before = begin;
+        if ((top_k == 0 || begin < top_k) && (double)f < p_ends && (counts[v] || (top_k > 0 && top_p < 1.0f)))
+        for (int o = begin; o < end; ++o) {
+            const int j = c.order[o];
+            const bool larger = c.key[j] > key || (c.key[j] == key && c.id[j] < id);
+            f += larger ? c.w[j] : 0ull;
+            before += larger ? 1 : 0;
+        }
+        rank[v] = before, front[v] = f;
+        if (before < top_k) kept += c.w[k];  // (weights below min-p among them)
+    }
+    // what top-k keeps: its weight is what top-p goes by
+    if (top_k > 0) {
+        (void)block_scan<kPickThreads>(kept, sh.wave_u, sum);
+        Z = (double)sum * 0x1p-52;
+    }
+    const double limit = (double)top_p * Z * 0x1p52, uncertain = slack * 0x1p52;
+    // Everything that stays is listed if top-k, top-p or min-p ends above the bound, or nothing below it has a weight.
+    // (The limit of top-p behind a top-k that the list does not hold is not known.)
+    const bool k_ends = all || (top_k > 0 && n >= top_k);
+    const bool ends = k_ends || ((top_k == 0 || top_p >= 1.0f) && ((top_p < 1.0f && (double)m_all >= limit) ||
+                                                                  (min_p > 0.0f && exp2_of(t_bound) < (double)min_p)));
+    bool unsure = !ends;
+    ArgPart stays[kEach], S;
+    kept = 0ull;
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) {
+        const int k = tid + v * kPickThreads;
+        stays[v] = 0ull;
+        if (k >= n) continue;
+        const double f = (double)front[v];
+        unsure = unsure || (top_p < 1.0f && slack > 0.0 && f > limit - uncertain && f < limit);
+        if ((top_k == 0 || rank[v] < top_k) && (top_p >= 1.0f || f < limit) && counts[v]) stays[v] = c.w[k];
+        kept += stays[v];
+    }
+    if (__syncthreads_or(unsure ? 1 : 0)) return put_on_list(has_sum && slack == 0.0 ? Z : 0.0);
+    // in the order of ids: buckets of ids, then the elements of the bucket where the running sum passes u S
+    const int id_shift = max(0, 32 - __builtin_clz((unsigned)max(V - 1, 1)) - 10);
+    for (int b = tid; b < kCandBuckets; b += kPickThreads) c.mass[b] = 0ull;
+    if (tid == 0) sh.n = -1, sh.token = -1, sh.last = 0;
+    (void)block_scan<kPickThreads>(kept, sh.wave_u, S);  // (with barriers inside)
+    const double target = (double)u * (double)S;
+#pragma unroll
+    for (int v = 0; v < kEach; ++v)
+        if (stays[v] != 0ull) atomicAdd(&c.mass[c.id[tid + v * kPickThreads] >> id_shift], stays[v]);
+    __syncthreads();
+    m_mine = 0ull;
+#pragma unroll
+    for (int v = 0; v < kPer; ++v) m[v] = c.mass[tid * kPer + v], m_mine += m[v];
+    m_front = block_scan<kPickThreads>(m_mine, sh.wave_u, m_all);
+#pragma unroll
+    for (int v = 0; v < kPer; ++v) {
+        c.mass[tid * kPer + v] = m_front;
+        if (m[v] > 0ull && (double)m_front <= target) atomicMax(&sh.n, tid * kPer + v);
+        m_front += m[v];
+    }
+    __syncthreads();
+    const int at = sh.n;
+    // (the bucket's elements: at most all)
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) {
+        const int k = tid + v * kPickThreads;
+        if (stays[v] != 0ull && (int)(c.id[k] >> id_shift) == at) c.order[atomicAdd(&sh.last, 1)] = (uint16_t)k;
+    }
+    __syncthreads();
+    const int in = sh.last;
+    const ArgPart base = c.mass[at];
+    // the last of them, by id, with at most the target in front of it
+    for (int o = tid; o < in; o += kPickThreads) {
+        const int k = c.order[o];
+        ArgPart f = base;
+        for (int j = 0; j < in; ++j) f += c.id[c.order[j]] < c.id[k] ? c.w[c.order[j]] : 0ull;
+        if ((double)f <= target) atomicMax(&sh.token, (int)c.id[k]);
+    }
+    __syncthreads();
+    put_token(sh.token, row, part, tokens);
+}
+
+// ---- rows on the list ----
+struct AgainShared {
+    union {
+        struct {
+            ArgPart mass[kHistBuckets];
+            uint32_t count[kHistBuckets];
+            ArgPart list[kCandidates];
+        } h;
+        struct {
+            ArgPart mass[kSteps], count[kSteps];  // of a step, later in front of it
+            ArgPart list[kCandidates];
+            ArgPart part[kSampleMaxV / kPart];
+        } s;
+        double chunk[kMaxChunks + kAgainThreads];
+    };
+    ArgPart wave_u[kAgainThreads / 64];
+    LocateShared<kAgainThreads> locate;
+    ArgPart found, base;
+    int n, token;
+};
+
+// n composites in falling order, padded with zeros to a power of two (n <= kCandidates, the size of the list).  A sorting
+// network: 66 steps of 60 cycles for 2048.  (Each compared with all others: 110 us for 1300.)
+__device__ void sort_falling(ArgPart *list, int n)
+{
+    constexpr int NT = kAgainThreads;
+    int size = 2;
+    while (size < n) size *= 2;
+    for (int k = n + (int)threadIdx.x; k < size; k += NT) list[k] = 0ull;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+        for (int d = run / 2; d >= 1; d /= 2) {
+            for (int k = threadIdx.x; k < size / 2; k += NT) {
+                const int i = 2 * k - (k & (d - 1)), j = i + d;  // (bit d of i is clear)
+                const ArgPart a = list[i], b = list[j];
+                if ((a < b) == ((i & run) == 0)) list[i] = b, list[j] = a;
+            }
+            __syncthreads();
+        }
+}
+// Of n composites (sorted here) the last one, in falling order, with less than `bound` in front of it, `front` included; value(k):
+// what the k-th of the order adds.  ~0 if there is none.
+template <class F>
+__device__ ArgPart last_in_order(ArgPart *list, int n, ArgPart front, double bound, F &&value, ArgPart *waves, ArgPart &found)
+{
+    constexpr int NT = kAgainThreads, kEach = kCandidates / NT;
+    sort_falling(list, n);
+    if (threadIdx.x == 0) found = ~0ull;
+    ArgPart v[kEach], mine = 0ull, all;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int k = (int)threadIdx.x * kEach + e;
+        v[e] = k < n ? value(list[k]) : 0ull;
+        mine += v[e];
+    }
+    ArgPart before = front + block_scan<NT>(mine, waves, all);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int k = (int)threadIdx.x * kEach + e;
+        if (k < n && (double)before < bound) atomicMin(&found, list[k]);
+        before += v[e];
+    }
+    __syncthreads();
+    const ArgPart r = found;
+    __syncthreads();
+    return r;
+}
+
+// The composite of the last element, in falling order, with less than `limit` in front of it: elements counted, or their
+// weights summed (in units of 1 / unit).  Elements below r.floor do not take part; r.floor if all stay.  However many
+// elements lie together: equal logits are told apart by their ids.
+template <bool MASS>
+__device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, AgainShared &sh)
+{
+    constexpr int NT = kAgainThreads;
     auto value = [&](double w) -> ArgPart { return MASS ? (ArgPart)(w * unit + 0.5) : 1ull; };
     auto bucket_of = [&](double t) { return min(kHistBuckets - 1, (int)(t * (kHistBuckets / kCut))); };
     const double bound = MASS ? limit * unit : limit;
@@ -412,9 +835,9 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, P
         };
         const int next = shift == 64 ? (bucket < 0 ? 64 : 53) : max(shift - 11, 0);
         const int width = shift - next;
-        for (int b = threadIdx.x; b < kHistBuckets; b += kPickThreads) sh.h.mass[b] = 0ull, sh.h.count[b] = 0u;
+        for (int b = threadIdx.x; b < kHistBuckets; b += NT) sh.h.mass[b] = 0ull, sh.h.count[b] = 0u;
         __syncthreads();
-        r.each([&](float v, int id) {
+        r.each<NT>([&](float v, int id) {
             const double t = r.log_weight(v);
             if (!left(v, id, t)) return;
             const int b = bucket < 0 ? bucket_of(t) : kHistBuckets - 1 - (int)((arg_part(v, id) >> next) & ((1ull << width) - 1ull));
@@ -422,7 +845,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, P
             if (MASS) atomicAdd(&sh.h.mass[b], value(exp2_of(t)));
         });
         __syncthreads();
-        constexpr int kPer = kHistBuckets / kPickThreads;
+        constexpr int kPer = kHistBuckets / NT;
         ArgPart v[kPer], mine = 0ull, total;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
@@ -430,14 +853,12 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, P
             v[u] = MASS ? sh.h.mass[b] : (ArgPart)sh.h.count[b];
             mine += v[u];
         }
-        ArgPart before = base + block_scan(mine, sh.wave_u, total);
-        if ((double)(base + total) < bound || total == 0ull) {
-            // (all of them stay.  Of a narrowed set only by the rounding of the weights' sum: the set's end is then the border)
-            if (bucket < 0) return r.floor;
-        }
+        ArgPart before = base + block_scan<NT>(mine, sh.wave_u, total);
+        if (bucket < 0 && (double)total < bound) return r.floor;  // all of them stay
         if (threadIdx.x == 0) sh.n = -1;
         __syncthreads();
         // the last bucket that holds elements and has less than the bound in front of it
+        const ArgPart first = before;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             if (sh.h.count[(int)threadIdx.x * kPer + u] > 0u && (double)before < bound) atomicMax(&sh.n, (int)threadIdx.x * kPer + u);
@@ -446,7 +867,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, P
         __syncthreads();
         const int at = sh.n;
         if (at < 0) return r.floor;
-        before -= mine;
+        before = first;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             if ((int)threadIdx.x * kPer + u == at) sh.base = before;
@@ -463,48 +884,42 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, P
         }
         if (members <= (uint32_t)kCandidates || shift == 0) {
             // few enough to be compared with one another
-            if (threadIdx.x == 0) sh.n = 0, sh.found = ~0ull;
+            if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
-            r.each([&](float v, int id) {
-                const double t = r.log_weight(v);
-                if (!left(v, id, t)) return;
+            r.each<NT>([&](float v, int id) {
+                if (!left(v, id, r.log_weight(v))) return;
                 const int k = atomicAdd(&sh.n, 1);
-                if (k < kCandidates) sh.h.list[k] = arg_part(v, id), sh.h.w[k] = value(MASS ? exp2_of(t) : 1.0);
+                if (k < kCandidates) sh.h.list[k] = arg_part(v, id);
             });
             __syncthreads();
             const int n = min(sh.n, kCandidates);
-            for (int k = threadIdx.x; k < n; k += kPickThreads) {
-                const ArgPart me = sh.h.list[k];
-                ArgPart front = base;
-                for (int o = 0; o < n; ++o) front += sh.h.list[o] > me ? sh.h.w[o] : 0ull;
-                if ((double)front < bound) atomicMin(&sh.found, me);
-            }
             __syncthreads();
-            const ArgPart found = sh.found;
-            __syncthreads();
+            const ArgPart found = last_in_order(sh.h.list, n, base, bound, [&](ArgPart c) {
+                return MASS ? value(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32))))) : 1ull; }, sh.wave_u, sh.found);
             return found == ~0ull ? r.floor : found;
         }
     }
 }
 
-// The row read again: thresholds, sums of chunks, token.
-__device__ int pick_again(PickRow r, int top_k, float top_p, float min_p, float u, PickShared &sh)
+// A row by one workgroup: thresholds, sums of chunks, token.  For rows whose border lies among thousands of equal logits.
+__device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float top_p, float min_p, float u, AgainShared &sh)
 {
+    constexpr int NT = kAgainThreads;
     double total;
     r.floor = 0ull, r.min_w = 0.0;
     __syncthreads();
     if (top_k > 0) r.floor = pick_threshold<false>(r, (double)top_k, 1.0, sh);
     if (top_p < 1.0f) {
         double mine = 0.0;
-        r.each([&](float v, int id) { mine += r.weight(v, id); });
-        (void)block_scan(mine, sh.wave_d, total);
+        r.each<NT>([&](float v, int id) { mine += r.weight(v, id); });
+        (void)block_scan<NT>(mine, sh.locate.wave_d, total);
         // as fine as sums below 2^62 allow
         const double unit = __builtin_amdgcn_ldexp(1.0, 61 - __builtin_amdgcn_frexp_exp(total));
         r.floor = pick_threshold<true>(r, (double)top_p * total, unit, sh);
     }
     r.min_w = (double)min_p;
     const int chunks = (r.V + kChunk - 1) / kChunk, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int k = wave; k < chunks; k += kPickThreads / 64) {
+    for (int k = wave; k < chunks; k += NT / 64) {
         const int start = k * kChunk, n = min(kChunk, r.V - start), a = behind_boundary(r.x + start);
         double sum = 0.0;
 #pragma unroll
@@ -518,19 +933,19 @@ __device__ int pick_again(PickRow r, int top_k, float top_p, float min_p, float 
         if (lane == 63) sh.chunk[k] = sum;
     }
     __syncthreads();
-    const int per = (chunks + kPickThreads - 1) / kPickThreads, from = (int)threadIdx.x * per, to = min(from + per, chunks);
+    const int per = (chunks + NT - 1) / NT, from = (int)threadIdx.x * per, to = min(from + per, chunks);
     double mine = 0.0;
     for (int k = from; k < to; ++k) mine += sh.chunk[k];
-    double before = block_scan(mine, sh.wave_d, total);
+    double before = block_scan<NT>(mine, sh.locate.wave_d, total);
     const double target = (double)u * total;
     if (threadIdx.x == 0) sh.n = -1;
     __syncthreads();
     // the last chunk with a weight that has at most the target in front of it
     for (int k = from; k < to; ++k) {
-        if (sh.chunk[k] > 0.0 && before <= target) atomicMax(&sh.n, k);
-        const double b = before;
-        before += sh.chunk[k];
-        sh.chunk[k] = b;  // from now on: the sum in front of it
+        const double w = sh.chunk[k];
+        if (w > 0.0 && before <= target) atomicMax(&sh.n, k);
+        sh.chunk[k] = before;  // from now on: the sum in front of it
+        before += w;
     }
     __syncthreads();
     const int k = sh.n;
@@ -538,265 +953,224 @@ __device__ int pick_again(PickRow r, int top_k, float top_p, float min_p, float 
     const double base = sh.chunk[k];
     __syncthreads();
     double c0, c1;
-    return pick_locate(r, k * kChunk, min(kChunk, r.V - k * kChunk), base, target, sh, c0, c1);
+    return pick_locate<NT>(r, k * kChunk, min(kChunk, r.V - k * kChunk), base, target, sh.locate, c0, c1);
 }
 
-__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
-    const float *__restrict__ logits, int T, int V, int seg_len, int segs, int hot_cap,
-    const int32_t *__restrict__ n_nodes, const float *__restrict__ uniforms, const SegStat *__restrict__ stat_all,
-    const ArgPart *__restrict__ hot_all, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
+// Step of the logit of an element with log-weight t, in falling order.
+__device__ __forceinline__ int step_of(double t) { return min(kSteps - 1, (int)(t * (kSteps / kCut))); }
+
+// Units of the integer weights of a row: as fine as sums below 2^62 allow.
+__device__ __forceinline__ double unit_of(double sum, int V)
 {
-    __shared__ PickShared sh;
-    const int tid = threadIdx.x, i = blockIdx.x, seq = blockIdx.y;
-    if (n_nodes && i > n_nodes[seq]) return;  // padding row
-    const size_t row = (size_t)seq * T + i;
-    const SegStat *const stat = stat_all + row * segs;
-    const ArgPart *const hot = hot_all + row * segs * (size_t)hot_cap;
-    const float tau = opt.tau[seq], top_p = opt.top_p[seq], min_p = opt.min_p[seq];
-    const int top_k = opt.top_k[seq];
-    // u from [0, 1): what is below, or no number, counts as 0, what is above as the largest float below 1
-    float u = uniforms[row];
-    const uint32_t ub = __float_as_uint(u);
-    u = ub > 0x7F800000u ? 0.0f : ub >= 0x3F800000u ? 0x1.fffffep-1f : u;
+    return __builtin_amdgcn_ldexp(1.0, 61 - (sum > 0.0 ? __builtin_amdgcn_frexp_exp(sum) : 32 - __builtin_clz((unsigned)V)));
+}
 
-    // the row's best, and the largest of the bounds (a list that is not complete: no bound holds)
-    ArgPart best = kNoPart;
-    uint32_t bound = 0u;
-    for (int s = tid; s < segs; s += kPickThreads) {
-        const ArgPart b = stat[s].best;
-        best = b > best ? b : best;
-        bound = max(bound, stat[s].listed > hot_cap ? ~0u : stat[s].bound);
-    }
-    best = wave_arg_max(best);
-    bound = ~wave_min_u32(~bound);
-    if ((tid & 63) == 63) sh.wave_u[tid >> 6] = best, sh.wave_d[tid >> 6] = (double)bound;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kPickThreads / 64; ++w) {
-        best = sh.wave_u[w] > best ? sh.wave_u[w] : best;
-        bound = max(bound, (uint32_t)sh.wave_d[w]);
-    }
-    __syncthreads();
-
-    auto done = [&](int token) {
-        if (tid == 0) {
-            if (tokens) tokens[row] = token;
-            else part[row] = 1ull << 32 | (uint32_t)~token;
+// The last workgroup of a row: the border from the steps' sums, the token.  False: too many elements in the border's step.
+__device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts, double unit, int top_k, float top_p, float min_p,
+                              float u, AgainShared &sh, int &token)
+{
+    constexpr int NT = kAgainThreads;
+    static_assert(NT >= kSteps, "a thread a step");
+    auto &s = sh.s;
+    const int tid = threadIdx.x;
+    // weight and count of each step over the row, then in front of it
+    ArgPart mass = 0ull, count = 0ull, mass_all, count_all;
+    if (tid < kSteps) {
+        for (int p = 0; p < parts; ++p) {
+            const StepSum *const q = steps + (size_t)p * (kSteps + 1) + tid;
+            mass += q[1].mass - q[0].mass, count += q[1].count - q[0].count;
         }
+    }
+    const ArgPart mass_front = block_scan<NT>(mass, sh.wave_u, mass_all), count_front = block_scan<NT>(count, sh.wave_u, count_all);
+    if (tid < kSteps) s.mass[tid] = mass_front, s.count[tid] = count_front;
+    // Elements of steps in front of `border` stay, those behind it do not; of it those from `floor` on with a weight of min_p.
+    int border = kSteps, n = 0;
+    ArgPart floor = 0ull;
+    auto last_below = [&](ArgPart front, bool holds, double limit) {  // the last step that holds elements with less than the limit in front
+        if (tid == 0) sh.n = -1;
+        __syncthreads();
+        if (tid < kSteps && holds && (double)front < limit) atomicMax(&sh.n, tid);
+        __syncthreads();
+        const int at = sh.n;
+        __syncthreads();
+        return at;
     };
-    if (best == kNoPart) return done(-1);
-    if (!(tau > 0.0f)) return done(arg_token(best));
-
-    PickRow r;
-    r.x = logits + row * (size_t)V;
-    r.V = V;
-    r.a = behind_boundary(r.x);
-    r.M = (double)key_float((uint32_t)(best >> 32));
-    r.c = 1.4426950408889634 / (double)tau;
-    r.floor = 0ull;
-    r.min_w = 0.0;
-    const bool filtered = top_k > 0 || top_p < 1.0f || min_p > 0.0f;
-    const bool has_sum = top_k == 0 && (top_p < 1.0f || !filtered);
-
-    // The row's sum.  A segment has also counted elements that are too small beside the row's best but not beside its own:
-    // `slack` bounds what they add (each is below 2^-40, if there are any).  A decision that this could change is left to
-    // the row read again.
-    double Z = 0.0, slack = 0.0;
-    if (has_sum) {
-        const int per = (segs + kPickThreads - 1) / kPickThreads, from = tid * per, to = min(from + per, segs);
-        double mine = 0.0;
-        bool doubt = false;
-        for (int s = from; s < to; ++s) {
-            double w = 0.0;
-            if (stat[s].best != kNoPart) {
-                const double t = r.log_weight(key_float((uint32_t)(stat[s].best >> 32)));
-                if (t >= kCut) {
-                    w = exp2_of(t) * stat[s].sum;
-                    doubt = doubt || !(r.log_weight(stat[s].low) >= kCut);
-                }
-            }
-            sh.seg[s] = w;
-            mine += w;
-        }
-        const double before = block_scan(mine, sh.wave_d, Z);
-        if (__syncthreads_or(doubt ? 1 : 0)) slack = (double)V * 0x1p-40;
-        if (!filtered) {
-            const double target = (double)u * Z;
-            if (tid == 0) sh.n = -1;
-            __syncthreads();
-            double b = before;
-            for (int s = from; s < to; ++s) {
-                if (sh.seg[s] > 0.0 && b <= target) atomicMax(&sh.n, s);
-                const double w = sh.seg[s];
-                sh.seg[s] = b;
-                b += w;
-            }
-            __syncthreads();
-            const int s = sh.n;
-            const double base = sh.seg[s];
-            __syncthreads();
-            double c0, c1;
-            int token = pick_locate(r, s * seg_len, min(seg_len, V - s * seg_len), base, target, sh, c0, c1);
-            if (slack > 0.0 && !(c0 <= (double)u * (Z - slack) && target < c1 - slack)) token = pick_again(r, 0, 1.0f, 0.0f, u, sh);
-            return done(token);
-        }
+    auto gather = [&](int step) {  // the step's elements that take part, into s.list and s.w; false: too many
+        if (tid == 0) sh.n = 0;
         __syncthreads();
-    }
-
-    // ---- the listed elements that reach the bound ----
-    auto &c = sh.c;
-    const uint32_t at_least = max(bound, kKeyOfNone + 1u);
-    if (tid == 0) sh.n = 0;
-    for (int b = tid; b < kCandBuckets; b += kPickThreads) c.mass[b] = 0ull, c.count[b] = 0u;
+        r.each<NT>([&](float v, int id) {
+            const double t = r.log_weight(v);
+            if (!(t >= kCut) || step_of(t) != step || arg_part(v, id) < floor) return;
+            const int k = atomicAdd(&sh.n, 1);
+            if (k < kCandidates) s.list[k] = arg_part(v, id);
+        });
+        __syncthreads();
+        n = sh.n;
+        __syncthreads();
+        return n <= kCandidates;
+    };
+    auto weight_of = [&](ArgPart c) { return (ArgPart)(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32)))) * unit + 0.5); };
+    // Of the gathered step the composite of the last element with less than `limit` in front of it.
+    auto last_in_step = [&](bool by_mass, ArgPart front, double limit) {
+        return last_in_order(s.list, n, front, limit, [&](ArgPart c) { return by_mass ? weight_of(c) : 1ull; }, sh.wave_u, sh.found);
+    };
+    // weight of the gathered elements from the floor on
+    auto weight_from_floor = [&]() {
+        ArgPart mine = 0ull, all;
+        for (int k = tid; k < n; k += NT) mine += s.list[k] >= floor ? weight_of(s.list[k]) : 0ull;
+        (void)block_scan<NT>(mine, sh.wave_u, all);
+        return all;
+    };
     __syncthreads();
-    if (bound != ~0u) {
-        for (int k = tid; k < segs * hot_cap; k += kPickThreads) {
-            const int s = k / hot_cap, e = k - s * hot_cap;
-            if (e < stat[s].listed) {
-                const ArgPart h = hot[k];
-                if ((uint32_t)(h >> 32) >= at_least) {
-                    const int at = atomicAdd(&sh.n, 1);
-                    if (at < kCandidates) c.key[at] = (uint32_t)(h >> 32), c.id[at] = (uint32_t)arg_token(h);
-                }
-            }
+    ArgPart kept = mass_all;  // weight of what top-k keeps
+    if (top_k > 0 && count_all > (ArgPart)top_k) {
+        border = last_below(count_front, count > 0ull, (double)top_k);
+        if (!gather(border)) return false;
+        floor = last_in_step(false, s.count[border], (double)top_k);
+        kept = s.mass[border] + weight_from_floor();
+    }
+    if (top_p < 1.0f) {
+        const double limit = (double)top_p * (double)kept;
+        const int at = min(border, last_below(mass_front, count > 0ull, limit));
+        if (at < border) {
+            border = at;
+            floor = 0ull;
+            if (!gather(border)) return false;
         }
+        const ArgPart found = last_in_step(true, s.mass[border], limit);
+        if (found != ~0ull && found > floor) floor = found;
+    }
+    if (min_p > 0.0f) {
+        const int at = step_of(fmax(log2((double)min_p), kCut));
+        if (at < border) {
+            border = at;
+            floor = 0ull;
+            if (!gather(border)) return false;
+        }
+    }
+    auto stays = [&](float v, int id) -> ArgPart {
+        const double t = r.log_weight(v);
+        if (!(t >= kCut)) return 0ull;
+        const int step = step_of(t);
+        if (step > border || (step == border && arg_part(v, id) < floor)) return 0ull;
+        const double weight = exp2_of(t);
+        return step == border && weight < (double)min_p ? 0ull : (ArgPart)(weight * unit + 0.5);
+    };
+    // ---- weights of the parts: steps in front of the border, and the border's elements ----
+    for (int p = tid; p < parts; p += NT) s.part[p] = steps[(size_t)p * (kSteps + 1) + border].mass;
+    __syncthreads();
+    if (border < kSteps)
+        for (int k = tid; k < n; k += NT) {
+            const int id = arg_token(s.list[k]);
+            const ArgPart w = stays(key_float((uint32_t)(s.list[k] >> 32)), id);
+            if (w != 0ull) atomicAdd(&s.part[id / kPart], w);
+        }
+    __syncthreads();
+    const int per = (parts + NT - 1) / NT, from = tid * per, to = min(from + per, parts);
+    ArgPart mine = 0ull, S, total;
+    for (int p = from; p < to; ++p) mine += s.part[p];
+    ArgPart before = block_scan<NT>(mine, sh.wave_u, S);
+    const double target = (double)u * (double)S;
+    if (tid == 0) sh.n = -1;
+    __syncthreads();
+    // the last part with a weight that has at most the target in front of it, then the last such element
+    for (int p = from; p < to; ++p) {
+        const ArgPart w = s.part[p];
+        if (w > 0ull && (double)before <= target) atomicMax(&sh.n, p);
+        s.part[p] = before;
+        before += w;
     }
     __syncthreads();
-    const int n = sh.n;
-    bool again = bound == ~0u || n > kCandidates;
-    // (below the bound nothing has a weight: the list is all there is)
-    const double t_bound = bound == 0u ? -1e30 : again ? 0.0 : r.log_weight(key_float(bound));
-    const bool all = bound == 0u || t_bound < kCut;
-    if (!again) {
-        // buckets in falling order: equal steps between the best and the least listed (for elements without a weight, the last)
-        const double span = fmax(all ? kCut : t_bound, kCut);
-        const double step = span < 0.0 ? (double)(kCandBuckets - 1) / span : 0.0;
-        auto bucket = [&](uint32_t key) { return min(kCandBuckets - 1, max(0, (int)(fmax(r.log_weight(key_float(key)), 2.0 * kCut) * step))); };
-        for (int k = tid; k < n; k += kPickThreads) {
-            const double t = r.log_weight(key_float(c.key[k]));
-            const ArgPart w = t >= kCut ? (ArgPart)(exp2_of(t) * 0x1p52 + 0.5) : 0ull;
-            c.w[k] = w;
-            const int b = bucket(c.key[k]);
-            atomicAdd(&c.mass[b], w);
-            atomicAdd(&c.count[b], 1u);
-        }
-        __syncthreads();
-        constexpr int kPer = kCandBuckets / kPickThreads;
-        ArgPart m[kPer], q[kPer], m_mine = 0ull, q_mine = 0ull, m_all, q_all;
+    const int p = sh.n;
+    const ArgPart base = s.part[p];
+    constexpr int kEach = kPart / NT;
+    const int id0 = p * kPart + tid * kEach;
+    ArgPart w[kEach];
+    mine = 0ull;
 #pragma unroll
-        for (int v = 0; v < kPer; ++v) {
-            m[v] = c.mass[tid * kPer + v], q[v] = c.count[tid * kPer + v];
-            m_mine += m[v], q_mine += q[v];
-        }
-        ArgPart m_front = block_scan(m_mine, sh.wave_u, m_all), q_front = block_scan(q_mine, sh.wave_u, q_all);
+    for (int g = 0; g < kEach; g += 4) {
+        const float4 x = load_four(r.x + id0 + g, r.V - id0 - g);
+        const float e[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int v = 0; v < kPer; ++v) {
-            c.mass[tid * kPer + v] = m_front, c.cursor[tid * kPer + v] = (uint32_t)q_front;
-            m_front += m[v], q_front += q[v];
+        for (int v = 0; v < 4; ++v) {
+            w[g + v] = e[v] > -INFINITY ? stays(e[v], id0 + g + v) : 0ull;
+            mine += w[g + v];
         }
-        __syncthreads();
-        for (int k = tid; k < n; k += kPickThreads) c.order[atomicAdd(&c.cursor[bucket(c.key[k])], 1u)] = (uint16_t)k;
-        __syncthreads();
-        // rank and weight in front of each, of at most kCandidates / kPickThreads elements a thread
-        constexpr int kEach = kCandidates / kPickThreads;
-        int rank[kEach];
-        ArgPart front[kEach];
+    }
+    before = base + block_scan<NT>(mine, sh.wave_u, total);
+    if (tid == 0) sh.token = -1;
+    __syncthreads();
 #pragma unroll
-        for (int v = 0; v < kEach; ++v) {
-            const int k = tid + v * kPickThreads;
-            rank[v] = 0, front[v] = 0ull;
-            if (k >= n) continue;
-            const int b = bucket(c.key[k]), end = (int)c.cursor[b], begin = end - (int)c.count[b];
-            ArgPart f = c.mass[b];
-            int before = begin;
-            for (int o = begin; o < end; ++o) {
-                const int j = c.order[o];
-                const bool larger = c.key[j] > c.key[k] || (c.key[j] == c.key[k] && c.id[j] < c.id[k]);
-                f += larger ? c.w[j] : 0ull;
-                before += larger ? 1 : 0;
-            }
-            rank[v] = before, front[v] = f;
-        }
-        // what top-k keeps, and its weight
-        if (top_k > 0) {
-            ArgPart kept = 0ull, sum;
+    for (int e = 0; e < kEach; ++e) {
+        if (w[e] > 0ull && (double)before <= target) atomicMax(&sh.token, id0 + e);
+        before += w[e];
+    }
+    __syncthreads();
+    token = sh.token;
+    return true;
+}
+
+// The rows on the list: kPart elements at a time, the last workgroup of a row to come draws its token.  Rows past `slots`
+// (the room for the steps' sums) and those with thousands of elements in one step are left to one workgroup each.
+__global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
+    const float *__restrict__ logits, int T, int V, int parts, int slots, const float *__restrict__ uniforms, const uint32_t *n_hard,
+    HardRow *hard, StepSum *steps, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
+{
+    __shared__ AgainShared sh;
+    constexpr int NT = kAgainThreads;
+    const int tid = threadIdx.x;
+    const int n = (int)*n_hard, shared = min(n, slots), items = shared * parts + (n - shared);
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const bool alone = item >= shared * parts;
+        const int h = alone ? shared + (item - shared * parts) : item / parts, p = alone ? 0 : item - h * parts;
+        const size_t row = (size_t)hard[h].row;
+        const int seq = (int)(row / T), top_k = opt.top_k[seq];
+        const float top_p = opt.top_p[seq], min_p = opt.min_p[seq], u = clean_uniform(uniforms[row]);
+        const double unit = unit_of(hard[h].sum, V);
+        const PickRow r = pick_row(logits, row, V, hard[h].best, opt.tau[seq]);
+        int token = -1;
+        bool found = false;
+        __syncthreads();  // (the shared memory of the item before)
+        if (!alone) {
+            auto &s = sh.s;
+            const int start = p * kPart, m = min(kPart, V - start), a = behind_boundary(r.x + start);
+            if (tid < kSteps) s.mass[tid] = 0ull, s.count[tid] = 0ull;
+            float4 x[kPart / (4 * NT) + 1];
 #pragma unroll
-            for (int v = 0; v < kEach; ++v)
-                if (tid + v * kPickThreads < n && rank[v] < top_k) kept += c.w[tid + v * kPickThreads];
-            (void)block_scan(kept, sh.wave_u, sum);
-            Z = (double)sum * 0x1p-52;
-        }
-        const double limit = (double)top_p * Z * 0x1p52, doubt = slack * 0x1p52;
-        // Everything that stays is listed if top-k, top-p or min-p ends above the bound, or nothing below it has a weight.
-        // (The limit of top-p behind a top-k that the list does not hold is not known.)
-        const bool k_ends = all || (top_k > 0 && n >= top_k);
-        const bool ends = k_ends || ((top_k == 0 || top_p >= 1.0f) && ((top_p < 1.0f && (double)m_all >= limit) ||
-                                                                      (min_p > 0.0f && exp2_of(t_bound) < (double)min_p)));
-        bool unsure = false;
-        ArgPart stays[kEach], kept = 0ull, S;
-#pragma unroll
-        for (int v = 0; v < kEach; ++v) {
-            const int k = tid + v * kPickThreads;
-            stays[v] = 0ull;
-            if (k >= n) continue;
-            const double f = (double)front[v];
-            unsure = unsure || (top_p < 1.0f && slack > 0.0 && f > limit - doubt && f < limit);
-            const double t = r.log_weight(key_float(c.key[k]));
-            if ((top_k == 0 || rank[v] < top_k) && (top_p >= 1.0f || f < limit) && t >= kCut &&
-                (min_p == 0.0f || exp2_of(t) >= (double)min_p))
-                stays[v] = c.w[k];
-            kept += stays[v];
-        }
-        if (__syncthreads_or((unsure || !ends) ? 1 : 0)) {
-            again = true;
-        } else {
-            // in the order of ids: buckets of ids, then the elements of the bucket where the running sum passes u S
-            (void)block_scan(kept, sh.wave_u, S);
-            const double target = (double)u * (double)S;
-            const int id_shift = max(0, 32 - __builtin_clz((unsigned)max(V - 1, 1)) - 10);
-            for (int b = tid; b < kCandBuckets; b += kPickThreads) c.mass[b] = 0ull;
-            if (tid == 0) sh.n = -1, sh.token = -1, sh.last = 0;
+            for (int g = 0; g < kPart / (4 * NT) + 1; ++g) x[g] = load_group(r.x + start, g * NT + tid, a, m);
             __syncthreads();
 #pragma unroll
-            for (int v = 0; v < kEach; ++v)
-                if (stays[v] != 0ull) atomicAdd(&c.mass[c.id[tid + v * kPickThreads] >> id_shift], stays[v]);
-            __syncthreads();
-            m_mine = 0ull;
+            for (int g = 0; g < kPart / (4 * NT) + 1; ++g) {
+                const float e[4] = {x[g].x, x[g].y, x[g].z, x[g].w};
 #pragma unroll
-            for (int v = 0; v < kPer; ++v) m[v] = c.mass[tid * kPer + v], m_mine += m[v];
-            m_front = block_scan(m_mine, sh.wave_u, m_all);
-#pragma unroll
-            for (int v = 0; v < kPer; ++v) {
-                c.mass[tid * kPer + v] = m_front;
-                if (m[v] > 0ull && (double)m_front <= target) atomicMax(&sh.n, tid * kPer + v);
-                m_front += m[v];
-            }
-            __syncthreads();
-            const int at = sh.n;
-            // (the bucket's elements: at most all)
-#pragma unroll
-            for (int v = 0; v < kEach; ++v) {
-                const int k = tid + v * kPickThreads;
-                if (stays[v] != 0ull && (int)(c.id[k] >> id_shift) == at) {
-                    const int o = atomicAdd(&sh.last, 1);
-                    c.order[o] = (uint16_t)k;
+                for (int v = 0; v < 4; ++v) {
+                    const double t = e[v] > -INFINITY ? r.log_weight(e[v]) : 2.0 * kCut;
+                    if (!(t >= kCut)) continue;
+                    const int step = step_of(t);
+                    atomicAdd(&s.mass[step], (ArgPart)(exp2_of(t) * unit + 0.5));
+                    atomicAdd(&s.count[step], 1ull);
                 }
             }
             __syncthreads();
-            const int in = sh.last;
-            const ArgPart base = c.mass[at];
-            // the last of them, by id, with at most the target in front of it
-            for (int o = tid; o < in; o += kPickThreads) {
-                const int k = c.order[o];
-                ArgPart f = base;
-                for (int j = 0; j < in; ++j) f += c.id[c.order[j]] < c.id[k] ? c.w[c.order[j]] : 0ull;
-                if ((double)f <= target) atomicMax(&sh.token, (int)c.id[k]);
-            }
+            ArgPart mass_all, count_all;
+            const ArgPart mass = block_scan<NT>(tid < kSteps ? s.mass[tid] : 0ull, sh.wave_u, mass_all);
+            const ArgPart count = block_scan<NT>(tid < kSteps ? s.count[tid] : 0ull, sh.wave_u, count_all);
+            StepSum *const out = steps + ((size_t)h * parts + p) * (kSteps + 1);
+            if (tid <= kSteps) out[tid] = tid < kSteps ? StepSum{mass, count} : StepSum{mass_all, count_all};
+            // what was written is visible to whoever sees the count that follows
+            __threadfence();
             __syncthreads();
-            return done(sh.token);
+            if (tid == 0) sh.n = atomicAdd(&hard[h].arrived, 1);
+            __syncthreads();
+            const bool last = sh.n == parts - 1;
+            __syncthreads();
+            if (!last) continue;
+            __threadfence();
+            found = pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit, top_k, top_p, min_p, u, sh, token);
         }
+        if (!found) token = pick_alone(r, top_k, top_p, min_p, u, sh);
+        put_token(token, row, part, tokens);
     }
-    if (again) done(pick_again(r, top_k, top_p, min_p, u, sh));
 }
 
 // Segments tile a row, a thread's registers hold them wherever the row starts, and the scratch of a shape covers
@@ -809,10 +1183,12 @@ int sample_selftest_host()
                 const SamplePlan p = sample_plan(batch, T, V);
                 if ((long long)(p.segs - 1) * p.seg_len >= V || (long long)p.segs * p.seg_len < V || p.segs > kMaxSegs) return 10031;
                 if (p.seg_len + 3 > p.vecs * kScanThreads * 4 || (p.vecs != 2 && p.vecs != 6)) return 10032;
-                if (p.hot_cap < p.hot_rank || p.hot_rank > kScanThreads) return 10033;
+                if (p.hot_cap < p.hot || p.hot > kScanThreads) return 10033;
                 const size_t per = (size_t)batch * T * p.segs;
-                if (p.hot_off < per * sizeof(SegStat) || p.part_off < p.hot_off + per * p.hot_cap * 8 || p.bytes < p.part_off + (size_t)batch * T * 8 ||
-                    ((p.hot_off | p.part_off) & 255u))
+                if (p.hot_off < per * sizeof(SegStat) || p.part_off < p.hot_off + per * p.hot_cap * 8 || p.hard_off < p.part_off + (size_t)batch * T * 8 ||
+                    p.step_off < p.hard_off + 256 + (size_t)batch * T * sizeof(HardRow) ||
+                    p.bytes < p.step_off + (size_t)p.slots * p.parts * (kSteps + 1) * sizeof(StepSum) ||
+                    (long long)p.parts * kPart < V || ((p.hot_off | p.part_off | p.hard_off | p.step_off) & 255u))
                     return 10034;
                 const size_t have = sample_scratch_upper(batch, T, V);
                 for (int b = 1; b <= batch; b += 1 + b / 2)
@@ -863,11 +1239,17 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
     SegStat *const stat = reinterpret_cast<SegStat *>(ws + p.stat_off);
     ArgPart *const hot = reinterpret_cast<ArgPart *>(ws + p.hot_off);
     *part = reinterpret_cast<ArgPart *>(ws + p.part_off);
+    uint32_t *const n_hard = reinterpret_cast<uint32_t *>(ws + p.hard_off);
+    HardRow *const hard = reinterpret_cast<HardRow *>(ws + p.hard_off + 256);
+    StepSum *const steps = reinterpret_cast<StepSum *>(ws + p.step_off);
     auto *scan = p.vecs == 2 ? sample_scan_kernel<2> : sample_scan_kernel<6>;
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_SCAN, st, scan, dim3(p.segs, T, batch), dim3(kScanThreads), 0, st, logits, T, V, p.seg_len, p.segs,
-               p.hot_rank, p.hot_cap, n_nodes, stat, hot, opt);
+               p.hot, p.hot_cap, n_nodes, stat, hot, n_hard, opt);
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_PICK, st, sample_pick_kernel, dim3(T, batch), dim3(kPickThreads), 0, st, logits, T, V, p.seg_len, p.segs,
-               p.hot_cap, n_nodes, uniforms, stat, hot, *part, tokens, opt);
+               p.hot_cap, n_nodes, uniforms, stat, hot, *part, tokens, n_hard, hard, opt);
+    // (a row goes on the list by what its logits are: the launch looks whether there are any)
+    DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_AGAIN, st, sample_again_kernel, dim3(kAgainGrid), dim3(kAgainThreads), 0, st, logits, T, V, p.parts, p.slots,
+               uniforms, n_hard, hard, steps, *part, tokens, opt);
     return launch_status();
 }
 
