@@ -16,9 +16,10 @@
 //          from one more read of the segment.  With filters: what stays is mostly among the listed elements above the
 //          largest of the segments' bounds (about 1200 of a row): their ranks and the weights in front of them from
 //          buckets.  A row of which that does not hold (thousands of tokens stay) is put on a list.
-//   again  what is on the list, many workgroups a row: each leaves, for 4096 elements, the count and the weight in front
-//          of each of 256 steps of the logit; the last one to come adds them up, reads the row once more for the elements
-//          of the one step where the border lies, and draws the token.
+//   steps, again   what is on the list.  First many workgroups a row: each leaves, for 8192 elements, the weight (and the number) in
+//          front of each of 256 steps of the logit.  Then one: it adds them up, reads the row once more for the elements
+//          of the one step where the border lies, and draws the token.  (In one launch, the last workgroup of a row going on
+//          by itself, the fences between the XCDs' caches took 20 times as long as the work.)
 // Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 62 bits allow):
 // their order does not matter.
 #include <algorithm>
@@ -29,10 +30,12 @@ namespace ddt {
 
 constexpr int kScanThreads = 256;
 constexpr int kPickThreads = 256;
+constexpr int kStepThreads = 512;
 constexpr int kAgainThreads = 512;
-constexpr int kAgainGrid = 512;     // workgroups that look for rows on the list
+constexpr int kStepGrid = 1024, kAgainGrid = 256;  // workgroups that look for rows on the list
 constexpr int kPart = 8192;         // elements of a row that a workgroup takes at a time there
 constexpr int kSteps = 256;         // steps of the logit
+constexpr int kStepList = 4096;     // elements of one step that are put in order
 constexpr int kSlots = 256;         // rows on the list that many workgroups take
 constexpr int kCandidates = 2048;   // listed elements that one row's pick holds
 constexpr int kCandBuckets = 1024;
@@ -67,21 +70,22 @@ struct SamplePlan {
 // A row on the list, and what is known of it.
 struct HardRow {
     double sum, best;   // of its weights (0: not known), its largest logit
-    int32_t row, arrived;
+    double scale;       // steps of the logit for a log-weight
+    int32_t row, pad;
 };
 // In front of each step of the logit, over kPart elements: their weights and their number.
 struct StepSum {
     ArgPart mass, count;
 };
 
-// Segments of 6140 elements, 24 a thread with room for a row that starts inside a 16-byte group; of 2044 where those make
+// Segments of 6144 elements, 24 a thread; of 2048 where those make
 // fewer than two workgroups a compute unit.  The lists together hold about 1400 of a row's largest, enough for the usual top-k.
 static SamplePlan sample_plan(int batch, int T, int V)
 {
     SamplePlan p{};
     const long long rows = (long long)batch * T;
-    p.vecs = rows * ((V + 6139) / 6140) < 512 && V <= 2044ll * kMaxSegs ? 2 : 6;
-    p.seg_len = p.vecs * 1024 - 4;
+    p.vecs = rows * ((V + 6143) / 6144) < 512 && V <= 2048ll * kMaxSegs ? 2 : 6;
+    p.seg_len = p.vecs * 1024;
     p.segs = (V + p.seg_len - 1) / p.seg_len;
     p.hot = std::min(200, std::max(16, 1400 / p.segs));
     p.hot_cap = 64;
@@ -106,7 +110,7 @@ size_t sample_scratch_upper(int batch, int T, int V)
     if (V > kSampleMaxV) V = kSampleMaxV;
     // (a segment's list is at most four times what 1400 divided by the segments asks for, or 64; short segments only below 512
     // workgroups of long ones)
-    const size_t long_segs = rows * ((V + 6139) / 6140), short_segs = std::min<size_t>(rows * ((V + 2043) / 2044), 512 * 4 + rows);
+    const size_t long_segs = rows * ((V + 6143) / 6144), short_segs = std::min<size_t>(rows * ((V + 2047) / 2048), 512 * 4 + rows);
     const size_t segs = std::max(long_segs, short_segs);
     most = segs * (sizeof(SegStat) + 64 * 8) + rows * (size_t)(4 * 1600) * 8 + rows * (8 + sizeof(HardRow)) + 2048 +
            std::min<size_t>(rows, kSlots) * ((V + kPart - 1) / kPart) * ((kSteps + 1) * sizeof(StepSum));
@@ -116,8 +120,10 @@ size_t sample_scratch_upper(int batch, int T, int V)
 // 2^t for t <= 0: 2^f, f within half of 0, from its interpolation at ten Chebyshev nodes (6e-16 off); 1 at 0 exactly.
 __device__ __forceinline__ double exp2_of(double t)
 {
+    // (rounded by the addition of 1.5 2^52, whose low word is then the integer: the conversions and v_ldexp_f64 take four times
+    // an addition's time)
     t = fmax(t, -64.0);
-    const double n = __builtin_rint(t), f = t - n;
+    const double shifted = t + 0x1.8p52, f = t - (shifted - 0x1.8p52);
     double p = 0x1.e5e9f548e5725p-28;
     p = fma(p, f, 0x1.b6571de2f2351p-24);
     p = fma(p, f, 0x1.62bfe46117445p-20);
@@ -129,7 +135,7 @@ __device__ __forceinline__ double exp2_of(double t)
     p = fma(p, f, 0x1.ebfbdff82c590p-3);
     p = fma(p, f, 0x1.62e42fefa39f7p-1);
     p = fma(p, f, 1.0);
-    return __builtin_amdgcn_ldexp(p, (int)n);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
 }
 
 // What counts as a logit: NaN as -inf (never selected), +inf as the largest finite number.
@@ -142,23 +148,34 @@ __device__ __forceinline__ float clean(float x)
 }
 constexpr uint32_t kKeyOfNone = 0x007FFFFFu;  // float_key(-inf)
 
-// Elements 4 v - a .. of `n` at p; a: elements that p is behind a 16-byte boundary.
-__device__ __forceinline__ float4 load_group(const float *p, int v, int a, int n)
-{
-    const int e = 4 * v - a;
-    float4 x;
-    if (e >= 0 && e + 3 < n) {
-        x = *reinterpret_cast<const float4 *>(p + e);
-    } else {
-        x.x = e >= 0 && e < n ? p[e] : -INFINITY;
-        x.y = e + 1 >= 0 && e + 1 < n ? p[e + 1] : -INFINITY;
-        x.z = e + 2 >= 0 && e + 2 < n ? p[e + 2] : -INFINITY;
-        x.w = e + 3 >= 0 && e + 3 < n ? p[e + 3] : -INFINITY;
+// A run of elements as the 16-byte groups inside it and up to six elements at its edges: thread e < head has element e, thread 4 + e
+// element head + 4 groups + e.  (Groups are loaded at clamped places and masked afterwards: under a branch each load would
+// be waited for before the next one, 44 us for a scan that takes 30.)
+struct Run {
+    const float *p;
+    int n, head, groups;
+    __device__ __forceinline__ Run(const float *from, int len) : p(from), n(len)
+    {
+        head = min(n, (int)((4 - ((reinterpret_cast<uintptr_t>(p) >> 2) & 3)) & 3));
+        groups = (n - head) >> 2;
     }
-    x.x = clean(x.x), x.y = clean(x.y), x.z = clean(x.z), x.w = clean(x.w);
-    return x;
-}
-__device__ __forceinline__ int behind_boundary(const float *p) { return (int)((reinterpret_cast<uintptr_t>(p) >> 2) & 3); }
+    __device__ __forceinline__ int id(int g) const { return head + 4 * g; }
+    __device__ __forceinline__ float4 load(int g) const  // (groups > 0)
+    {
+        return reinterpret_cast<const float4 *>(p + head)[min(g, groups - 1)];
+    }
+    __device__ __forceinline__ void four(int g, const float4 &x, float (&e)[4]) const
+    {
+        const bool in = g < groups;
+        e[0] = in ? clean(x.x) : -INFINITY, e[1] = in ? clean(x.y) : -INFINITY;
+        e[2] = in ? clean(x.z) : -INFINITY, e[3] = in ? clean(x.w) : -INFINITY;
+    }
+    __device__ __forceinline__ int edge_id() const
+    {
+        const int t = threadIdx.x;
+        return t < 4 ? (t < head ? t : -1) : t < 8 && head + 4 * groups + (t - 4) < n ? head + 4 * groups + (t - 4) : -1;
+    }
+};
 
 template <int VECS>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
@@ -179,13 +196,16 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
     const size_t row = (size_t)seq * T + i;
     const int start = seg * seg_len, n = min(seg_len, V - start);
     const float *const p = logits + row * (size_t)V + start;
-    const int a = behind_boundary(p);
+    const Run run(p, n);
+    float4 raw[VECS];
+    if (run.groups > 0)
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) raw[j] = run.load(j * kScanThreads + tid);
+    const int edge = run.edge_id();
+    const float at_edge = edge >= 0 ? clean(p[edge]) : -INFINITY;
     float x[VECS][4];
 #pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        const float4 v = load_group(p, j * kScanThreads + tid, a, n);
-        x[j][0] = v.x, x[j][1] = v.y, x[j][2] = v.z, x[j][3] = v.w;
-    }
+    for (int j = 0; j < VECS; ++j) run.four(j * kScanThreads + tid, raw[j], x[j]);
     const float tau = opt.tau[seq];
     const bool filtered = opt.top_k[seq] > 0 || opt.top_p[seq] < 1.0f || opt.min_p[seq] > 0.0f;
     // the sum of the row: where nothing is filtered, and where top-p goes by it
@@ -200,10 +220,17 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
         for (int e = 0; e < 4; ++e) {
             const bool more = x[j][e] > bv;
             bv = more ? x[j][e] : bv;
-            bi = more ? 4 * (j * kScanThreads + tid) - a + e : bi;
+            bi = more ? run.id(j * kScanThreads + tid) + e : bi;
             alive += x[j][e] > -INFINITY ? 1 : 0;
         }
-    const ArgPart mine = wave_arg_max(bv > -INFINITY ? arg_part(bv, start + bi) : kNoPart);
+    ArgPart mine = bv > -INFINITY ? arg_part(bv, start + bi) : kNoPart;
+    if (at_edge > -INFINITY) {
+        const ArgPart o = arg_part(at_edge, start + edge);
+        mine = o > mine ? o : mine;
+        bv = fmaxf(bv, at_edge);
+        ++alive;
+    }
+    mine = wave_arg_max(mine);
     if (lane == 63) s_best[wave] = mine;
     s_max[tid] = bv;
     alive = wave_scan_inclusive_i32(alive);
@@ -218,15 +245,17 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
         const double m = (double)key_float((uint32_t)(best >> 32)), c = 1.4426950408889634 / (double)tau;
         double sum = 0.0;
         float low = INFINITY;
+        auto add = [&](float v) {
+            const double t = ((double)v - m) * c;
+            const bool counts = t >= kCut;
+            sum += counts ? exp2_of(t) : 0.0;
+            low = counts ? fminf(low, v) : low;
+        };
 #pragma unroll
         for (int j = 0; j < VECS; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const double t = ((double)x[j][e] - m) * c;
-                const bool counts = t >= kCut;
-                sum += counts ? exp2_of(t) : 0.0;
-                low = counts ? fminf(low, x[j][e]) : low;
-            }
+            for (int e = 0; e < 4; ++e) add(x[j][e]);
+        if (wave == 0) add(at_edge);
         sum = wave_sum_f64_lane63(sum);
         low = -wave_max_f32(-low);
         if (lane == 63) s_sum[wave] = sum, s_low[wave] = low;
@@ -284,9 +313,13 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
                 const unsigned long long who = __builtin_amdgcn_ballot_w64(x[j][e] >= least);
                 if (who == 0ull) continue;
                 const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
-                if (x[j][e] >= least && mine < hot_cap) list[mine] = arg_part(x[j][e], start + 4 * (j * kScanThreads + tid) - a + e);
+                if (x[j][e] >= least && mine < hot_cap) list[mine] = arg_part(x[j][e], start + run.id(j * kScanThreads + tid) + e);
                 at += __popcll(who);
             }
+        if (at_edge >= least) {
+            const int mine = atomicAdd(&s_listed, 1);
+            if (mine < hot_cap) list[mine] = arg_part(at_edge, start + edge);
+        }
         __syncthreads();
     }
     if (tid == 0) {
@@ -348,10 +381,13 @@ __device__ __forceinline__ X block_scan(X v, X *waves, X &total)
 // A row, and what stays of it as far as that is known.
 struct PickRow {
     const float *x;
-    int V, a;
+    int V;
     double M, c;       // largest logit, log2(e) / tau
     ArgPart floor;     // composites below it do not stay
     double min_w;      // nor do weights below this one
+    double scale;      // steps of the logit for a log-weight
+    // step of an element with log-weight t, in falling order
+    __device__ __forceinline__ int step_of(double t) const { return min(kSteps - 1, (int)(t * scale)); }
     __device__ __forceinline__ double log_weight(float v) const { return ((double)v - M) * c; }
     // weight of element id if it stays, else 0
     __device__ __forceinline__ double weight(float v, int id) const
@@ -361,23 +397,40 @@ struct PickRow {
         const double w = exp2_of(t);
         return w >= min_w ? w : 0.0;
     }
+    // f(value, id) for every element from lo to hi (lo > -inf)
     template <int NT, class F>
-    __device__ __forceinline__ void each(F &&f) const
+    __device__ __forceinline__ void each(float lo, float hi, F &&f) const
     {
-        constexpr int kAhead = 4;
-        const int groups = (V + a + 3) >> 2;
-        for (int g = threadIdx.x; g < groups; g += kAhead * NT) {
+        constexpr int kAhead = 8;
+        const Run run(x, V);
+        for (int g = threadIdx.x; g < run.groups; g += kAhead * NT) {
             float4 p[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) p[u] = load_group(x, g + u * NT, a, V);
+            for (int u = 0; u < kAhead; ++u) p[u] = run.load(g + u * NT);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const float e[4] = {p[u].x, p[u].y, p[u].z, p[u].w};
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (e[v] > -INFINITY) f(e[v], 4 * (g + u * NT) - a + v);
+                float e[4];
+                run.four(g + u * NT, p[u], e);
+                // (most groups have none)
+                const float top = fmaxf(fmaxf(e[0] <= hi ? e[0] : -INFINITY, e[1] <= hi ? e[1] : -INFINITY),
+                                        fmaxf(e[2] <= hi ? e[2] : -INFINITY, e[3] <= hi ? e[3] : -INFINITY));
+                if (!(top >= lo)) continue;
+#pragma unroll 1
+                for (int v = 0; v < 4; ++v) {
+                    const float y = v == 0 ? e[0] : v == 1 ? e[1] : v == 2 ? e[2] : e[3];
+                    if (y >= lo && y <= hi) f(y, run.id(g + u * NT) + v);
+                }
             }
         }
+        const int edge = run.edge_id();
+        const float v = edge >= 0 ? clean(x[edge]) : -INFINITY;
+        if (v >= lo && v <= hi) f(v, edge);
+    }
+    // A logit whose log-weight is at least t, and whose neighbours' are not far below: what `each` is to look at
+    __device__ __forceinline__ float about(double t, double side) const
+    {
+        const double v = M + t / c;
+        return (float)fmax(-3.4028234e38, fmin(3.4028234e38, v + side * (1e-5 * (fabs(v) + fabs(M)) + 1e-30)));
     }
 };
 __device__ __forceinline__ PickRow pick_row(const float *logits, size_t row, int V, double M, float tau)
@@ -385,27 +438,32 @@ __device__ __forceinline__ PickRow pick_row(const float *logits, size_t row, int
     PickRow r;
     r.x = logits + row * (size_t)V;
     r.V = V;
-    r.a = behind_boundary(r.x);
     r.M = M;
     r.c = 1.4426950408889634 / (double)tau;
     r.floor = 0ull;
     r.min_w = 0.0;
+    r.scale = kSteps / kCut;
     return r;
 }
-// Four elements at p, of which n > 0 are there.  (Rows of any length: 4-byte alignment.)
-__device__ __forceinline__ float4 load_four(const float *p, int n)
+// Elements [from, to) of a row, at most 4 G of them, -inf behind them.  (From any place: loads of 16 bytes on 4-byte boundaries, all
+// requested before any is looked at; the last ones of the row one by one.)
+template <int G>
+__device__ __forceinline__ void load_run(const float *x, int V, int from, int to, float (&e)[4 * G])
 {
     typedef float four __attribute__((ext_vector_type(4), aligned(4)));
-    float4 x = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    if (n >= 4) {
-        const four f = *reinterpret_cast<const four *>(p);
-        x = make_float4(clean(f.x), clean(f.y), clean(f.z), clean(f.w));
-    } else {
-        if (n > 0) x.x = clean(p[0]);
-        if (n > 1) x.y = clean(p[1]);
-        if (n > 2) x.z = clean(p[2]);
+    four f[G];
+    if (V >= 4)
+#pragma unroll
+        for (int g = 0; g < G; ++g) f[g] = *reinterpret_cast<const four *>(x + max(0, min(from + 4 * g, V - 4)));
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) e[4 * g + v] = from + 4 * g + v < to ? clean(f[g][v]) : -INFINITY;
+    if (to > V - 4 && from < to) {  // (at most a few threads)
+#pragma unroll
+        for (int k = 0; k < 4 * G; ++k)
+            if ((from + (k & ~3) > V - 4) && from + k < to) e[k] = clean(x[from + k]);
     }
-    return x;
 }
 // u from [0, 1): what is below, or no number, counts as 0, what is above as the largest float below 1
 __device__ __forceinline__ float clean_uniform(float u)
@@ -434,15 +492,15 @@ __device__ int pick_locate(const PickRow &r, int start, int n, double base, doub
     const int per = ((n + NT - 1) / NT + 3) / 4 * 4, from = start + (int)threadIdx.x * per, to = min(from + per, start + n);
     double mine = 0.0, total;
     int last = -1;
-    for (int g = from; g < to; g += 4) {
-        const float4 p = load_four(r.x + g, to - g);
-        const float e[4] = {p.x, p.y, p.z, p.w};
+    constexpr int G = NT == kPickThreads ? 6 : 1;  // groups of a thread: a segment by `pick`, a chunk by `again`
+    static_assert(4 * G * NT >= (NT == kPickThreads ? 6144 : kChunk), "the run fits");
+    float x[4 * G];
+    load_run<G>(r.x, r.V, from, to, x);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const double w = e[u] > -INFINITY ? r.weight(e[u], g + u) : 0.0;
-            if (w > 0.0) last = g + u;
-            mine += w;
-        }
+    for (int k = 0; k < 4 * G; ++k) {
+        const double w = x[k] > -INFINITY ? r.weight(x[k], from + k) : 0.0;
+        if (w > 0.0) last = from + k;
+        mine += w;
     }
     if (threadIdx.x == 0) sh.last = -1, sh.token = -1;
     const double before = base + block_scan<NT>(mine, sh.wave_d, total);
@@ -542,7 +600,12 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
     const bool has_sum = top_k == 0 && (top_p < 1.0f || !filtered);
     double Z = 0.0;
     auto put_on_list = [&](double sum) {
-        if (tid == 0) hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, (int32_t)row, 0};
+        if (tid != 0) return;
+        // Where the sum is known and top-p is the first filter, its border lies above log-weights of which all V elements would
+        // not make up half of what it leaves out: the steps go that far only
+        double deep = -kCut;
+        if (sum > 0.0 && top_p < 1.0f) deep = fmin(deep, fmax(1.0, log2((double)V / ((1.0 - (double)top_p) * sum)) + 2.0));
+        hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, -kSteps / deep, (int32_t)row, 0};
     };
 
     // The row's sum.  A segment has also counted elements that are too small beside the row's best but not beside its own:
@@ -755,8 +818,8 @@ struct AgainShared {
             ArgPart list[kCandidates];
         } h;
         struct {
-            ArgPart mass[kSteps], count[kSteps];  // of a step, later in front of it
-            ArgPart list[kCandidates];
+            ArgPart mass[kSteps], count[kSteps];  // in front of a step
+            ArgPart list[kStepList];
             ArgPart part[kSampleMaxV / kPart];
         } s;
         double chunk[kMaxChunks + kAgainThreads];
@@ -767,7 +830,7 @@ struct AgainShared {
     int n, token;
 };
 
-// n composites in falling order, padded with zeros to a power of two (n <= kCandidates, the size of the list).  A sorting
+// n composites in falling order, padded with zeros to a power of two (the list's size is one).  A sorting
 // network: 66 steps of 60 cycles for 2048.  (Each compared with all others: 110 us for 1300.)
 __device__ void sort_falling(ArgPart *list, int n)
 {
@@ -788,10 +851,10 @@ __device__ void sort_falling(ArgPart *list, int n)
 }
 // Of n composites (sorted here) the last one, in falling order, with less than `bound` in front of it, `front` included; value(k):
 // what the k-th of the order adds.  ~0 if there is none.
-template <class F>
+template <int N, class F>
 __device__ ArgPart last_in_order(ArgPart *list, int n, ArgPart front, double bound, F &&value, ArgPart *waves, ArgPart &found)
 {
-    constexpr int NT = kAgainThreads, kEach = kCandidates / NT;
+    constexpr int NT = kAgainThreads, kEach = N / NT;  // n <= N
     sort_falling(list, n);
     if (threadIdx.x == 0) found = ~0ull;
     ArgPart v[kEach], mine = 0ull, all;
@@ -837,7 +900,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
         const int width = shift - next;
         for (int b = threadIdx.x; b < kHistBuckets; b += NT) sh.h.mass[b] = 0ull, sh.h.count[b] = 0u;
         __syncthreads();
-        r.each<NT>([&](float v, int id) {
+        r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) {
             const double t = r.log_weight(v);
             if (!left(v, id, t)) return;
             const int b = bucket < 0 ? bucket_of(t) : kHistBuckets - 1 - (int)((arg_part(v, id) >> next) & ((1ull << width) - 1ull));
@@ -886,7 +949,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
             // few enough to be compared with one another
             if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
-            r.each<NT>([&](float v, int id) {
+            r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) {
                 if (!left(v, id, r.log_weight(v))) return;
                 const int k = atomicAdd(&sh.n, 1);
                 if (k < kCandidates) sh.h.list[k] = arg_part(v, id);
@@ -894,7 +957,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
             __syncthreads();
             const int n = min(sh.n, kCandidates);
             __syncthreads();
-            const ArgPart found = last_in_order(sh.h.list, n, base, bound, [&](ArgPart c) {
+            const ArgPart found = last_in_order<kCandidates>(sh.h.list, n, base, bound, [&](ArgPart c) {
                 return MASS ? value(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32))))) : 1ull; }, sh.wave_u, sh.found);
             return found == ~0ull ? r.floor : found;
         }
@@ -911,7 +974,7 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     if (top_k > 0) r.floor = pick_threshold<false>(r, (double)top_k, 1.0, sh);
     if (top_p < 1.0f) {
         double mine = 0.0;
-        r.each<NT>([&](float v, int id) { mine += r.weight(v, id); });
+        r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) { mine += r.weight(v, id); });
         (void)block_scan<NT>(mine, sh.locate.wave_d, total);
         // as fine as sums below 2^62 allow
         const double unit = __builtin_amdgcn_ldexp(1.0, 61 - __builtin_amdgcn_frexp_exp(total));
@@ -920,15 +983,12 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     r.min_w = (double)min_p;
     const int chunks = (r.V + kChunk - 1) / kChunk, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int k = wave; k < chunks; k += NT / 64) {
-        const int start = k * kChunk, n = min(kChunk, r.V - start), a = behind_boundary(r.x + start);
+        const int start = k * kChunk, from = start + lane * (kChunk / 64);
         double sum = 0.0;
+        float x[kChunk / 64];
+        load_run<kChunk / 256>(r.x, r.V, from, min(from + kChunk / 64, r.V), x);
 #pragma unroll
-        for (int g = 0; g < kChunk / 256 + 1; ++g) {  // (one group more where the chunk starts inside one)
-            if (4 * (g * 64) - a >= n) break;
-            const float4 p = load_group(r.x + start, g * 64 + lane, a, n);
-            const int id = start + 4 * (g * 64 + lane) - a;
-            sum += (r.weight(p.x, id) + r.weight(p.y, id + 1)) + (r.weight(p.z, id + 2) + r.weight(p.w, id + 3));
-        }
+        for (int e = 0; e < kChunk / 64; ++e) sum += x[e] > -INFINITY ? r.weight(x[e], from + e) : 0.0;
         sum = wave_sum_f64_lane63(sum);
         if (lane == 63) sh.chunk[k] = sum;
     }
@@ -956,9 +1016,6 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     return pick_locate<NT>(r, k * kChunk, min(kChunk, r.V - k * kChunk), base, target, sh.locate, c0, c1);
 }
 
-// Step of the logit of an element with log-weight t, in falling order.
-__device__ __forceinline__ int step_of(double t) { return min(kSteps - 1, (int)(t * (kSteps / kCut))); }
-
 // Units of the integer weights of a row: as fine as sums below 2^62 allow.
 __device__ __forceinline__ double unit_of(double sum, int V)
 {
@@ -976,9 +1033,18 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     // weight and count of each step over the row, then in front of it
     ArgPart mass = 0ull, count = 0ull, mass_all, count_all;
     if (tid < kSteps) {
-        for (int p = 0; p < parts; ++p) {
-            const StepSum *const q = steps + (size_t)p * (kSteps + 1) + tid;
-            mass += q[1].mass - q[0].mass, count += q[1].count - q[0].count;
+        for (int p = 0; p < parts; p += 8) {
+            StepSum q[16];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                const StepSum *const at = steps + (size_t)min(p + v, parts - 1) * (kSteps + 1) + tid;
+                q[2 * v] = at[0], q[2 * v + 1] = at[1];
+            }
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                mass += p + v < parts ? q[2 * v + 1].mass - q[2 * v].mass : 0ull;
+                count += p + v < parts ? q[2 * v + 1].count - q[2 * v].count : 0ull;
+            }
         }
     }
     const ArgPart mass_front = block_scan<NT>(mass, sh.wave_u, mass_all), count_front = block_scan<NT>(count, sh.wave_u, count_all);
@@ -998,21 +1064,21 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     auto gather = [&](int step) {  // the step's elements that take part, into s.list and s.w; false: too many
         if (tid == 0) sh.n = 0;
         __syncthreads();
-        r.each<NT>([&](float v, int id) {
+        r.each<NT>(r.about(step == kSteps - 1 ? kCut : (step + 1) / r.scale, -1.0), r.about(step / r.scale, 1.0), [&](float v, int id) {
             const double t = r.log_weight(v);
-            if (!(t >= kCut) || step_of(t) != step || arg_part(v, id) < floor) return;
+            if (!(t >= kCut) || r.step_of(t) != step || arg_part(v, id) < floor) return;
             const int k = atomicAdd(&sh.n, 1);
-            if (k < kCandidates) s.list[k] = arg_part(v, id);
+            if (k < kStepList) s.list[k] = arg_part(v, id);
         });
         __syncthreads();
         n = sh.n;
         __syncthreads();
-        return n <= kCandidates;
+        return n <= kStepList;
     };
     auto weight_of = [&](ArgPart c) { return (ArgPart)(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32)))) * unit + 0.5); };
     // Of the gathered step the composite of the last element with less than `limit` in front of it.
     auto last_in_step = [&](bool by_mass, ArgPart front, double limit) {
-        return last_in_order(s.list, n, front, limit, [&](ArgPart c) { return by_mass ? weight_of(c) : 1ull; }, sh.wave_u, sh.found);
+        return last_in_order<kStepList>(s.list, n, front, limit, [&](ArgPart c) { return by_mass ? weight_of(c) : 1ull; }, sh.wave_u, sh.found);
     };
     // weight of the gathered elements from the floor on
     auto weight_from_floor = [&]() {
@@ -1021,37 +1087,40 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         (void)block_scan<NT>(mine, sh.wave_u, all);
         return all;
     };
-    __syncthreads();
+    // The step where min-p ends is known ahead; what ends behind it needs no closer look.
+    const int min_step = min_p > 0.0f ? r.step_of(fmax(log2((double)min_p), kCut)) : kSteps;
     ArgPart kept = mass_all;  // weight of what top-k keeps
     if (top_k > 0 && count_all > (ArgPart)top_k) {
-        border = last_below(count_front, count > 0ull, (double)top_k);
-        if (!gather(border)) return false;
-        floor = last_in_step(false, s.count[border], (double)top_k);
-        kept = s.mass[border] + weight_from_floor();
+        const int at = last_below(count_front, count > 0ull, (double)top_k);
+        if (at <= min_step || top_p < 1.0f) {
+            border = at;
+            if (!gather(border)) return false;
+            floor = last_in_step(false, s.count[border], (double)top_k);
+            kept = s.mass[border] + weight_from_floor();
+        }
     }
     if (top_p < 1.0f) {
         const double limit = (double)top_p * (double)kept;
-        const int at = min(border, last_below(mass_front, count > 0ull, limit));
-        if (at < border) {
-            border = at;
-            floor = 0ull;
-            if (!gather(border)) return false;
+        const int at = last_below(mass_front, mass > 0ull, limit);
+        if (at <= border && at <= min_step) {
+            if (at < border) {
+                border = at;
+                floor = 0ull;
+                if (!gather(border)) return false;
+                }
+            const ArgPart found = last_in_step(true, s.mass[border], limit);
+            if (found != ~0ull && found > floor) floor = found;
         }
-        const ArgPart found = last_in_step(true, s.mass[border], limit);
-        if (found != ~0ull && found > floor) floor = found;
     }
-    if (min_p > 0.0f) {
-        const int at = step_of(fmax(log2((double)min_p), kCut));
-        if (at < border) {
-            border = at;
-            floor = 0ull;
-            if (!gather(border)) return false;
-        }
+    if (min_step < border) {
+        border = min_step;
+        floor = 0ull;
+        if (!gather(border)) return false;
     }
     auto stays = [&](float v, int id) -> ArgPart {
         const double t = r.log_weight(v);
         if (!(t >= kCut)) return 0ull;
-        const int step = step_of(t);
+        const int step = r.step_of(t);
         if (step > border || (step == border && arg_part(v, id) < floor)) return 0ull;
         const double weight = exp2_of(t);
         return step == border && weight < (double)min_p ? 0ull : (ArgPart)(weight * unit + 0.5);
@@ -1087,15 +1156,12 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     const int id0 = p * kPart + tid * kEach;
     ArgPart w[kEach];
     mine = 0ull;
+    float x[kEach];
+    load_run<kEach / 4>(r.x, r.V, id0, min(id0 + kEach, r.V), x);
 #pragma unroll
-    for (int g = 0; g < kEach; g += 4) {
-        const float4 x = load_four(r.x + id0 + g, r.V - id0 - g);
-        const float e[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            w[g + v] = e[v] > -INFINITY ? stays(e[v], id0 + g + v) : 0ull;
-            mine += w[g + v];
-        }
+    for (int e = 0; e < kEach; ++e) {
+        w[e] = x[e] > -INFINITY ? stays(x[e], id0 + e) : 0ull;
+        mine += w[e];
     }
     before = base + block_scan<NT>(mine, sh.wave_u, total);
     if (tid == 0) sh.token = -1;
@@ -1110,66 +1176,80 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     return true;
 }
 
-// The rows on the list: kPart elements at a time, the last workgroup of a row to come draws its token.  Rows past `slots`
-// (the room for the steps' sums) and those with thousands of elements in one step are left to one workgroup each.
+// The rows on the list, kPart elements at a time: what lies in front of each step.
+__global__ __launch_bounds__(kStepThreads) void sample_steps_kernel(
+    const float *__restrict__ logits, int T, int V, int parts, int slots, const uint32_t *__restrict__ n_hard,
+    const HardRow *__restrict__ hard, StepSum *__restrict__ steps, SampleOpts opt)
+{
+    constexpr int NT = kStepThreads;
+    __shared__ ArgPart s_mass[kSteps], s_waves[NT / 64];
+    __shared__ uint32_t s_count[kSteps];
+    const int tid = threadIdx.x;
+    const int items = min((int)*n_hard, slots) * parts;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int h = item / parts, p = item - h * parts;
+        const HardRow row = hard[h];
+        const int seq = row.row / T;
+        const bool by_count = opt.top_k[seq] > 0;
+        const double unit = unit_of(row.sum, V);
+        PickRow r = pick_row(logits, (size_t)row.row, V, row.best, opt.tau[seq]);
+        r.scale = row.scale;
+        const int start = p * kPart;
+        const Run run(r.x + start, min(kPart, V - start));
+        constexpr int G = kPart / (4 * NT);
+        float4 x[G];
+        if (run.groups > 0)
+#pragma unroll
+            for (int g = 0; g < G; ++g) x[g] = run.load(g * NT + tid);
+        const int edge = run.edge_id();
+        const float at_edge = edge >= 0 ? clean(run.p[edge]) : -INFINITY;
+        __syncthreads();  // (the shared memory of the item before)
+        if (tid < kSteps) s_mass[tid] = 0ull, s_count[tid] = 0u;
+        __syncthreads();
+        auto add = [&](float v) {
+            const double t = v > -INFINITY ? r.log_weight(v) : 2.0 * kCut;
+            if (!(t >= kCut)) return;
+            const int step = r.step_of(t);
+            atomicAdd(&s_mass[step], (ArgPart)(exp2_of(t) * unit + 0.5));
+            if (by_count) atomicAdd(&s_count[step], 1u);
+        };
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float e[4];
+            run.four(g * NT + tid, x[g], e);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) add(e[v]);
+        }
+        if (tid < 64) add(at_edge);
+        __syncthreads();
+        ArgPart mass_all, count_all;
+        const ArgPart mass = block_scan<NT>(tid < kSteps ? s_mass[tid] : 0ull, s_waves, mass_all);
+        const ArgPart count = block_scan<NT>(tid < kSteps ? (ArgPart)s_count[tid] : 0ull, s_waves, count_all);
+        StepSum *const out = steps + ((size_t)h * parts + p) * (kSteps + 1);
+        if (tid <= kSteps) out[tid] = tid < kSteps ? StepSum{mass, count} : StepSum{mass_all, count_all};
+    }
+}
+
+// Then a workgroup a row.  Rows past `slots` (the room for the steps' sums) and those with thousands of elements in one
+// step are read as often as it takes.
 __global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
-    const float *__restrict__ logits, int T, int V, int parts, int slots, const float *__restrict__ uniforms, const uint32_t *n_hard,
-    HardRow *hard, StepSum *steps, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
+    const float *__restrict__ logits, int T, int V, int parts, int slots, const float *__restrict__ uniforms, const uint32_t *__restrict__ n_hard,
+    const HardRow *__restrict__ hard, const StepSum *__restrict__ steps, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
 {
     __shared__ AgainShared sh;
-    constexpr int NT = kAgainThreads;
-    const int tid = threadIdx.x;
-    const int n = (int)*n_hard, shared = min(n, slots), items = shared * parts + (n - shared);
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const bool alone = item >= shared * parts;
-        const int h = alone ? shared + (item - shared * parts) : item / parts, p = alone ? 0 : item - h * parts;
-        const size_t row = (size_t)hard[h].row;
-        const int seq = (int)(row / T), top_k = opt.top_k[seq];
-        const float top_p = opt.top_p[seq], min_p = opt.min_p[seq], u = clean_uniform(uniforms[row]);
-        const double unit = unit_of(hard[h].sum, V);
-        const PickRow r = pick_row(logits, row, V, hard[h].best, opt.tau[seq]);
+    const int n = (int)*n_hard;
+    for (int h = blockIdx.x; h < n; h += gridDim.x) {
+        const HardRow row = hard[h];
+        const int seq = row.row / T, top_k = opt.top_k[seq];
+        const float top_p = opt.top_p[seq], min_p = opt.min_p[seq], u = clean_uniform(uniforms[row.row]);
+        PickRow r = pick_row(logits, (size_t)row.row, V, row.best, opt.tau[seq]);
+        r.scale = row.scale;
         int token = -1;
-        bool found = false;
-        __syncthreads();  // (the shared memory of the item before)
-        if (!alone) {
-            auto &s = sh.s;
-            const int start = p * kPart, m = min(kPart, V - start), a = behind_boundary(r.x + start);
-            if (tid < kSteps) s.mass[tid] = 0ull, s.count[tid] = 0ull;
-            float4 x[kPart / (4 * NT) + 1];
-#pragma unroll
-            for (int g = 0; g < kPart / (4 * NT) + 1; ++g) x[g] = load_group(r.x + start, g * NT + tid, a, m);
-            __syncthreads();
-#pragma unroll
-            for (int g = 0; g < kPart / (4 * NT) + 1; ++g) {
-                const float e[4] = {x[g].x, x[g].y, x[g].z, x[g].w};
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const double t = e[v] > -INFINITY ? r.log_weight(e[v]) : 2.0 * kCut;
-                    if (!(t >= kCut)) continue;
-                    const int step = step_of(t);
-                    atomicAdd(&s.mass[step], (ArgPart)(exp2_of(t) * unit + 0.5));
-                    atomicAdd(&s.count[step], 1ull);
-                }
-            }
-            __syncthreads();
-            ArgPart mass_all, count_all;
-            const ArgPart mass = block_scan<NT>(tid < kSteps ? s.mass[tid] : 0ull, sh.wave_u, mass_all);
-            const ArgPart count = block_scan<NT>(tid < kSteps ? s.count[tid] : 0ull, sh.wave_u, count_all);
-            StepSum *const out = steps + ((size_t)h * parts + p) * (kSteps + 1);
-            if (tid <= kSteps) out[tid] = tid < kSteps ? StepSum{mass, count} : StepSum{mass_all, count_all};
-            // what was written is visible to whoever sees the count that follows
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) sh.n = atomicAdd(&hard[h].arrived, 1);
-            __syncthreads();
-            const bool last = sh.n == parts - 1;
-            __syncthreads();
-            if (!last) continue;
-            __threadfence();
-            found = pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit, top_k, top_p, min_p, u, sh, token);
-        }
-        if (!found) token = pick_alone(r, top_k, top_p, min_p, u, sh);
-        put_token(token, row, part, tokens);
+        __syncthreads();  // (the shared memory of the row before)
+        if (h >= slots ||
+            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit_of(row.sum, V), top_k, top_p, min_p, u, sh, token))
+            token = pick_alone(r, top_k, top_p, min_p, u, sh);
+        put_token(token, (size_t)row.row, part, tokens);
     }
 }
 
@@ -1182,7 +1262,7 @@ int sample_selftest_host()
             for (int batch : {1, 2, 5, 16, 64}) {
                 const SamplePlan p = sample_plan(batch, T, V);
                 if ((long long)(p.segs - 1) * p.seg_len >= V || (long long)p.segs * p.seg_len < V || p.segs > kMaxSegs) return 10031;
-                if (p.seg_len + 3 > p.vecs * kScanThreads * 4 || (p.vecs != 2 && p.vecs != 6)) return 10032;
+                if (p.seg_len > p.vecs * kScanThreads * 4 || (p.vecs != 2 && p.vecs != 6)) return 10032;
                 if (p.hot_cap < p.hot || p.hot > kScanThreads) return 10033;
                 const size_t per = (size_t)batch * T * p.segs;
                 if (p.hot_off < per * sizeof(SegStat) || p.part_off < p.hot_off + per * p.hot_cap * 8 || p.hard_off < p.part_off + (size_t)batch * T * 8 ||
@@ -1247,9 +1327,12 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
                p.hot, p.hot_cap, n_nodes, stat, hot, n_hard, opt);
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_PICK, st, sample_pick_kernel, dim3(T, batch), dim3(kPickThreads), 0, st, logits, T, V, p.seg_len, p.segs,
                p.hot_cap, n_nodes, uniforms, stat, hot, *part, tokens, n_hard, hard, opt);
-    // (a row goes on the list by what its logits are: the launch looks whether there are any)
-    DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_AGAIN, st, sample_again_kernel, dim3(kAgainGrid), dim3(kAgainThreads), 0, st, logits, T, V, p.parts, p.slots,
-               uniforms, n_hard, hard, steps, *part, tokens, opt);
+    // (a row goes on the list by what its logits are: these look whether there are any)
+    const int rows = batch * T, most = (int)std::min<long long>(kStepGrid, (long long)p.slots * p.parts);
+    DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_STEPS, st, sample_steps_kernel, dim3(most), dim3(kStepThreads), 0, st, logits, T, V, p.parts, p.slots,
+               n_hard, hard, steps, opt);
+    DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_AGAIN, st, sample_again_kernel, dim3(std::min(rows, kAgainGrid)), dim3(kAgainThreads), 0, st, logits, T, V,
+               p.parts, p.slots, uniforms, n_hard, hard, steps, *part, tokens, opt);
     return launch_status();
 }
 
