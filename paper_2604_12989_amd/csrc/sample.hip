@@ -378,6 +378,14 @@ __device__ __forceinline__ X block_scan(X v, X *waves, X &total)
     return before + up;
 }
 
+// The largest of the values of the lanes where `on`, which rise with the lane: one lane's atomic.  (64 lanes' atomics on one
+// address take the wave through a loop of 64 rounds: a search over 8192 elements 25 us, with this 3.)
+__device__ __forceinline__ void wave_last(int *out, bool on, int value)
+{
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(on);
+    if (who != 0ull && (int)(threadIdx.x & 63) == 63 - __builtin_clzll(who)) atomicMax(out, value);
+}
+
 // A row, and what stays of it as far as that is known.
 struct PickRow {
     const float *x;
@@ -397,9 +405,9 @@ struct PickRow {
         const double w = exp2_of(t);
         return w >= min_w ? w : 0.0;
     }
-    // f(value, id) for every element from lo to hi (lo > -inf)
+    // f(value, id) for every finite element
     template <int NT, class F>
-    __device__ __forceinline__ void each(float lo, float hi, F &&f) const
+    __device__ __forceinline__ void each(F &&f) const
     {
         constexpr int kAhead = 8;
         const Run run(x, V);
@@ -411,20 +419,59 @@ struct PickRow {
             for (int u = 0; u < kAhead; ++u) {
                 float e[4];
                 run.four(g + u * NT, p[u], e);
-                // (most groups have none)
-                const float top = fmaxf(fmaxf(e[0] <= hi ? e[0] : -INFINITY, e[1] <= hi ? e[1] : -INFINITY),
-                                        fmaxf(e[2] <= hi ? e[2] : -INFINITY, e[3] <= hi ? e[3] : -INFINITY));
-                if (!(top >= lo)) continue;
 #pragma unroll 1
                 for (int v = 0; v < 4; ++v) {
                     const float y = v == 0 ? e[0] : v == 1 ? e[1] : v == 2 ? e[2] : e[3];
-                    if (y >= lo && y <= hi) f(y, run.id(g + u * NT) + v);
+                    if (y > -INFINITY) f(y, run.id(g + u * NT) + v);
                 }
             }
         }
         const int edge = run.edge_id();
         const float v = edge >= 0 ? clean(x[edge]) : -INFINITY;
-        if (v >= lo && v <= hi) f(v, edge);
+        if (v > -INFINITY) f(v, edge);
+    }
+    // The composites of the elements from lo to hi (lo > -inf) into a list with room for `room`; their number, also where that is
+    // more, through n (0 before).  A wave takes its place in the list once for 2048 elements.
+    template <int NT>
+    __device__ __forceinline__ void collect(float lo, float hi, ArgPart *list, int room, int *n) const
+    {
+        constexpr int kAhead = 8;
+        const Run run(x, V);
+        const int lane = threadIdx.x & 63;
+        for (int g0 = (int)threadIdx.x - lane; g0 < run.groups; g0 += kAhead * NT) {  // (uniform over a wave)
+            float4 p[kAhead];
+            float e[kAhead][4];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) p[u] = run.load(g0 + lane + u * NT);
+            int hits = 0;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                run.four(g0 + lane + u * NT, p[u], e[u]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) hits += __popcll(__builtin_amdgcn_ballot_w64(e[u][v] >= lo && e[u][v] <= hi));
+            }
+            if (hits == 0) continue;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(n, hits);
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const bool hit = e[u][v] >= lo && e[u][v] <= hi;
+                    const unsigned long long who = __builtin_amdgcn_ballot_w64(hit);
+                    if (who == 0ull) continue;
+                    const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+                    if (hit && mine < room) list[mine] = arg_part(e[u][v], run.id(g0 + lane + u * NT) + v);
+                    at += __popcll(who);
+                }
+        }
+        const int edge = run.edge_id();
+        const float v = edge >= 0 ? clean(x[edge]) : -INFINITY;
+        if (v >= lo && v <= hi) {
+            const int mine = atomicAdd(n, 1);
+            if (mine < room) list[mine] = arg_part(v, edge);
+        }
     }
     // A logit whose log-weight is at least t, and whose neighbours' are not far below: what `each` is to look at
     __device__ __forceinline__ float about(double t, double side) const
@@ -504,8 +551,8 @@ __device__ int pick_locate(const PickRow &r, int start, int n, double base, doub
     }
     if (threadIdx.x == 0) sh.last = -1, sh.token = -1;
     const double before = base + block_scan<NT>(mine, sh.wave_d, total);
-    if (last >= 0) atomicMax(&sh.last, last);
-    if (last >= 0 && before <= target && target < before + mine) atomicMax(&sh.token, (int)threadIdx.x);
+    wave_last(&sh.last, last >= 0, last);
+    wave_last(&sh.token, last >= 0 && before <= target && target < before + mine, (int)threadIdx.x);
     __syncthreads();
     // (should rounding leave no such thread: the one that holds the last element)
     const int who = sh.token >= 0 ? sh.token : sh.last >= 0 ? (sh.last - start) / per : -1;
@@ -570,7 +617,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
     ulonglong2 ahead[kAhead];
 #pragma unroll
     for (int v = 0; v < kAhead; ++v)
-        if (tid + v * kPickThreads < slots) ahead[v] = reinterpret_cast<const ulonglong2 *>(hot)[tid + v * kPickThreads];
+        if (slots > 0) ahead[v] = reinterpret_cast<const ulonglong2 *>(hot)[min(tid + v * kPickThreads, slots - 1)];
 
     // the row's best, and the largest of the bounds (a list that is not complete: no bound holds)
     ArgPart best = kNoPart;
@@ -636,12 +683,14 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
             if (tid == 0) sh.n = -1;
             __syncthreads();
             double b = before;
+            int last = -1;
             for (int s = from; s < to; ++s) {
-                if (sh.seg[s] > 0.0 && b <= target) atomicMax(&sh.n, s);
                 const double w = sh.seg[s];
+                if (w > 0.0 && b <= target) last = s;
                 sh.seg[s] = b;
                 b += w;
             }
+            wave_last(&sh.n, last >= 0, last);
             __syncthreads();
             const int s = sh.n;
             const double base = sh.seg[s];
@@ -659,19 +708,44 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
     for (int b = tid; b < kCandBuckets; b += kPickThreads) c.mass[b] = 0ull, c.count[b] = 0u;
     __syncthreads();
     if (bound != ~0u) {
-        auto take = [&](ArgPart h) {
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < kCandidates) c.key[at] = (uint32_t)(h >> 32), c.id[at] = (uint32_t)arg_token(h);
-        };
-        auto look = [&](int pair, const ulonglong2 &h) {
+        auto look = [&](int pair, const ulonglong2 &h, bool &x, bool &y) {
             const int s = 2 * pair / hot_cap, left = sh.listed[s] - (2 * pair - s * hot_cap);
-            if (left > 0 && (uint32_t)(h.x >> 32) >= at_least) take(h.x);
-            if (left > 1 && (uint32_t)(h.y >> 32) >= at_least) take(h.y);
+            x = left > 0 && (uint32_t)(h.x >> 32) >= at_least;
+            y = left > 1 && (uint32_t)(h.y >> 32) >= at_least;
         };
+        // (a wave takes its places at once)
+        const int lane = tid & 63;
+        auto place = [&](int at, unsigned long long who, bool on, ArgPart h) {
+            const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+            if (on && mine < kCandidates) c.key[mine] = (uint32_t)(h >> 32), c.id[mine] = (uint32_t)arg_token(h);
+        };
+        for (int k0 = 0; k0 < slots; k0 += kAhead * kPickThreads) {
+            if (k0 > 0) {
 #pragma unroll
-        for (int v = 0; v < kAhead; ++v)
-            if (tid + v * kPickThreads < slots) look(tid + v * kPickThreads, ahead[v]);
-        for (int k = tid + kAhead * kPickThreads; k < slots; k += kPickThreads) look(k, reinterpret_cast<const ulonglong2 *>(hot)[k]);
+                for (int v = 0; v < kAhead; ++v)
+                    ahead[v] = reinterpret_cast<const ulonglong2 *>(hot)[min(k0 + tid + v * kPickThreads, slots - 1)];
+            }
+            bool x[kAhead], y[kAhead];
+            int hits = 0;
+#pragma unroll
+            for (int v = 0; v < kAhead; ++v) {
+                const int pair = k0 + tid + v * kPickThreads;
+                look(min(pair, slots - 1), ahead[v], x[v], y[v]);
+                x[v] = x[v] && pair < slots, y[v] = y[v] && pair < slots;
+                hits += __popcll(__builtin_amdgcn_ballot_w64(x[v])) + __popcll(__builtin_amdgcn_ballot_w64(y[v]));
+            }
+            int at = 0;
+            if (lane == 0 && hits > 0) at = atomicAdd(&sh.n, hits);
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int v = 0; v < kAhead; ++v) {
+                const unsigned long long wx = __builtin_amdgcn_ballot_w64(x[v]), wy = __builtin_amdgcn_ballot_w64(y[v]);
+                if (wx != 0ull) place(at, wx, x[v], ahead[v].x);
+                at += __popcll(wx);
+                if (wy != 0ull) place(at, wy, y[v], ahead[v].y);
+                at += __popcll(wy);
+            }
+        }
     }
     __syncthreads();
     const int n = sh.n;
@@ -781,12 +855,14 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
 #pragma unroll
     for (int v = 0; v < kPer; ++v) m[v] = c.mass[tid * kPer + v], m_mine += m[v];
     m_front = block_scan<kPickThreads>(m_mine, sh.wave_u, m_all);
+    int last = -1;
 #pragma unroll
     for (int v = 0; v < kPer; ++v) {
         c.mass[tid * kPer + v] = m_front;
-        if (m[v] > 0ull && (double)m_front <= target) atomicMax(&sh.n, tid * kPer + v);
+        if (m[v] > 0ull && (double)m_front <= target) last = tid * kPer + v;
         m_front += m[v];
     }
+    wave_last(&sh.n, last >= 0, last);
     __syncthreads();
     const int at = sh.n;
     // (the bucket's elements: at most all)
@@ -819,7 +895,7 @@ struct AgainShared {
         } h;
         struct {
             ArgPart mass[kSteps], count[kSteps];  // in front of a step
-            ArgPart list[kStepList];
+            ArgPart sub[kSteps], list[kStepList], few[kStepList];
             ArgPart part[kSampleMaxV / kPart];
         } s;
         double chunk[kMaxChunks + kAgainThreads];
@@ -856,21 +932,24 @@ __device__ ArgPart last_in_order(ArgPart *list, int n, ArgPart front, double bou
 {
     constexpr int NT = kAgainThreads, kEach = N / NT;  // n <= N
     sort_falling(list, n);
-    if (threadIdx.x == 0) found = ~0ull;
-    ArgPart v[kEach], mine = 0ull, all;
+    ArgPart v[kEach], mine = 0ull, all, last = 0ull;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
         const int k = (int)threadIdx.x * kEach + e;
-        v[e] = k < n ? value(list[k]) : 0ull;
+        v[e] = k < n && list[k] != 0ull ? value(list[k]) : 0ull;
         mine += v[e];
     }
-    ArgPart before = front + block_scan<NT>(mine, waves, all);
+    if (threadIdx.x == 0) found = ~0ull;
+    ArgPart before = front + block_scan<NT>(mine, waves, all);  // (with barriers inside)
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
         const int k = (int)threadIdx.x * kEach + e;
-        if (k < n && (double)before < bound) atomicMin(&found, list[k]);
+        if (k < n && list[k] != 0ull && (double)before < bound) last = list[k];
         before += v[e];
     }
+    // (falling order: the least of the threads' last ones; a wave's is that of its last lane that has any)
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(last != 0ull);
+    if (who != 0ull && (int)(threadIdx.x & 63) == 63 - __builtin_clzll(who)) atomicMin(&found, last);
     __syncthreads();
     const ArgPart r = found;
     __syncthreads();
@@ -900,7 +979,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
         const int width = shift - next;
         for (int b = threadIdx.x; b < kHistBuckets; b += NT) sh.h.mass[b] = 0ull, sh.h.count[b] = 0u;
         __syncthreads();
-        r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) {
+        r.each<NT>([&](float v, int id) {
             const double t = r.log_weight(v);
             if (!left(v, id, t)) return;
             const int b = bucket < 0 ? bucket_of(t) : kHistBuckets - 1 - (int)((arg_part(v, id) >> next) & ((1ull << width) - 1ull));
@@ -922,11 +1001,13 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
         __syncthreads();
         // the last bucket that holds elements and has less than the bound in front of it
         const ArgPart first = before;
+        int last = -1;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
-            if (sh.h.count[(int)threadIdx.x * kPer + u] > 0u && (double)before < bound) atomicMax(&sh.n, (int)threadIdx.x * kPer + u);
+            if (sh.h.count[(int)threadIdx.x * kPer + u] > 0u && (double)before < bound) last = (int)threadIdx.x * kPer + u;
             before += v[u];
         }
+        wave_last(&sh.n, last >= 0, last);
         __syncthreads();
         const int at = sh.n;
         if (at < 0) return r.floor;
@@ -949,7 +1030,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
             // few enough to be compared with one another
             if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
-            r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) {
+            r.each<NT>([&](float v, int id) {
                 if (!left(v, id, r.log_weight(v))) return;
                 const int k = atomicAdd(&sh.n, 1);
                 if (k < kCandidates) sh.h.list[k] = arg_part(v, id);
@@ -974,7 +1055,7 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     if (top_k > 0) r.floor = pick_threshold<false>(r, (double)top_k, 1.0, sh);
     if (top_p < 1.0f) {
         double mine = 0.0;
-        r.each<NT>(-3.4028235e38f, 3.4028235e38f, [&](float v, int id) { mine += r.weight(v, id); });
+        r.each<NT>([&](float v, int id) { mine += r.weight(v, id); });
         (void)block_scan<NT>(mine, sh.locate.wave_d, total);
         // as fine as sums below 2^62 allow
         const double unit = __builtin_amdgcn_ldexp(1.0, 61 - __builtin_amdgcn_frexp_exp(total));
@@ -1001,12 +1082,14 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     if (threadIdx.x == 0) sh.n = -1;
     __syncthreads();
     // the last chunk with a weight that has at most the target in front of it
+    int last = -1;
     for (int k = from; k < to; ++k) {
         const double w = sh.chunk[k];
-        if (w > 0.0 && before <= target) atomicMax(&sh.n, k);
+        if (w > 0.0 && before <= target) last = k;
         sh.chunk[k] = before;  // from now on: the sum in front of it
         before += w;
     }
+    wave_last(&sh.n, last >= 0, last);
     __syncthreads();
     const int k = sh.n;
     if (k < 0) return -1;
@@ -1055,35 +1138,66 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     auto last_below = [&](ArgPart front, bool holds, double limit) {  // the last step that holds elements with less than the limit in front
         if (tid == 0) sh.n = -1;
         __syncthreads();
-        if (tid < kSteps && holds && (double)front < limit) atomicMax(&sh.n, tid);
+        wave_last(&sh.n, tid < kSteps && holds && (double)front < limit, tid);
         __syncthreads();
         const int at = sh.n;
         __syncthreads();
         return at;
     };
-    auto gather = [&](int step) {  // the step's elements that take part, into s.list and s.w; false: too many
+    auto gather = [&](int step) {  // the step's elements that take part, into s.list, anything else there as 0; false: too many
         if (tid == 0) sh.n = 0;
         __syncthreads();
-        r.each<NT>(r.about(step == kSteps - 1 ? kCut : (step + 1) / r.scale, -1.0), r.about(step / r.scale, 1.0), [&](float v, int id) {
-            const double t = r.log_weight(v);
-            if (!(t >= kCut) || r.step_of(t) != step || arg_part(v, id) < floor) return;
-            const int k = atomicAdd(&sh.n, 1);
-            if (k < kStepList) s.list[k] = arg_part(v, id);
-        });
+        r.collect<NT>(r.about(step == kSteps - 1 ? kCut : (step + 1) / r.scale, -1.0), r.about(step / r.scale, 1.0), s.list, kStepList, &sh.n);
         __syncthreads();
         n = sh.n;
         __syncthreads();
-        return n <= kStepList;
+        if (n > kStepList) return false;
+        for (int k = tid; k < n; k += NT) {
+            const double t = r.log_weight(key_float((uint32_t)(s.list[k] >> 32)));
+            if (!(t >= kCut) || r.step_of(t) != step || s.list[k] < floor) s.list[k] = 0ull;
+        }
+        __syncthreads();
+        return true;
     };
     auto weight_of = [&](ArgPart c) { return (ArgPart)(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32)))) * unit + 0.5); };
-    // Of the gathered step the composite of the last element with less than `limit` in front of it.
+    // Of the gathered step the composite of the last element with less than `limit` in front of it: once more by steps, 256 of
+    // the step, and the elements of one of those against one another.
+    auto sub_step = [&](ArgPart c) {
+        const double t = r.log_weight(key_float((uint32_t)(c >> 32))) * r.scale;
+        return max(0, min(kSteps - 1, (int)((t - (double)border) * kSteps)));
+    };
     auto last_in_step = [&](bool by_mass, ArgPart front, double limit) {
-        return last_in_order<kStepList>(s.list, n, front, limit, [&](ArgPart c) { return by_mass ? weight_of(c) : 1ull; }, sh.wave_u, sh.found);
+        if (tid < kSteps) s.sub[tid] = 0ull;
+        if (tid == 0) sh.n = 0, sh.found = ~0ull;
+        __syncthreads();
+        for (int k = tid; k < n; k += NT)
+            if (s.list[k] != 0ull) atomicAdd(&s.sub[sub_step(s.list[k])], by_mass ? weight_of(s.list[k]) : 1ull);
+        __syncthreads();
+        ArgPart all;
+        const ArgPart own = tid < kSteps ? s.sub[tid] : 0ull, before = front + block_scan<NT>(own, sh.wave_u, all);
+        const int at = last_below(before, own > 0ull, limit);
+        if (tid == at) sh.base = before;
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        for (int k = tid; k < n; k += NT)
+            if (s.list[k] != 0ull && sub_step(s.list[k]) == at) s.few[atomicAdd(&sh.n, 1)] = s.list[k];
+        __syncthreads();
+        const int m = sh.n;
+        const ArgPart base = sh.base;
+        for (int k = tid; k < m; k += NT) {
+            ArgPart f = base;
+            for (int o = 0; o < m; ++o) f += s.few[o] > s.few[k] ? (by_mass ? weight_of(s.few[o]) : 1ull) : 0ull;
+            if ((double)f < limit) atomicMin(&sh.found, s.few[k]);
+        }
+        __syncthreads();
+        const ArgPart found = sh.found;
+        __syncthreads();
+        return found;
     };
     // weight of the gathered elements from the floor on
     auto weight_from_floor = [&]() {
         ArgPart mine = 0ull, all;
-        for (int k = tid; k < n; k += NT) mine += s.list[k] >= floor ? weight_of(s.list[k]) : 0ull;
+        for (int k = tid; k < n; k += NT) mine += s.list[k] != 0ull && s.list[k] >= floor ? weight_of(s.list[k]) : 0ull;
         (void)block_scan<NT>(mine, sh.wave_u, all);
         return all;
     };
@@ -1130,6 +1244,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     __syncthreads();
     if (border < kSteps)
         for (int k = tid; k < n; k += NT) {
+            if (s.list[k] == 0ull) continue;
             const int id = arg_token(s.list[k]);
             const ArgPart w = stays(key_float((uint32_t)(s.list[k] >> 32)), id);
             if (w != 0ull) atomicAdd(&s.part[id / kPart], w);
@@ -1143,12 +1258,14 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     if (tid == 0) sh.n = -1;
     __syncthreads();
     // the last part with a weight that has at most the target in front of it, then the last such element
+    int last = -1;
     for (int p = from; p < to; ++p) {
         const ArgPart w = s.part[p];
-        if (w > 0ull && (double)before <= target) atomicMax(&sh.n, p);
+        if (w > 0ull && (double)before <= target) last = p;
         s.part[p] = before;
         before += w;
     }
+    wave_last(&sh.n, last >= 0, last);
     __syncthreads();
     const int p = sh.n;
     const ArgPart base = s.part[p];
@@ -1166,11 +1283,13 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     before = base + block_scan<NT>(mine, sh.wave_u, total);
     if (tid == 0) sh.token = -1;
     __syncthreads();
+    last = -1;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        if (w[e] > 0ull && (double)before <= target) atomicMax(&sh.token, id0 + e);
+        if (w[e] > 0ull && (double)before <= target) last = id0 + e;
         before += w[e];
     }
+    wave_last(&sh.token, last >= 0, last);
     __syncthreads();
     token = sh.token;
     return true;
