@@ -322,8 +322,11 @@ int ddtree_q4_load(const void *k_codes, const void *k_scales, const void *v_code
  * ddtree_verify_attn_spans over a 4-bit cache: sequence s owns its rows kv_start[s] .. kv_start[s] + kv_len[s] - 1
  * (below cache_rows), whose keys and values are what the codes stand for; the tree rows are tensors of dtype, as there.
  * T = 1 with the one bit of the mask set is a plain decoding step: the token sees the cache and itself.
- * Arguments otherwise, precision and workspace as in ddtree_verify_attn; D a multiple of 32.
+ * Arguments otherwise, precision and workspace as in ddtree_verify_attn (its own size for one shape:
+ * ddtree_verify_attn_q4_workspace_bytes, as ddtree_verify_attn_workspace_bytes is for that call); D a multiple of 32.
  */
+size_t ddtree_verify_attn_q4_workspace_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype,
+                                             long long sum_L);
 int ddtree_verify_attn_q4(const void *q, const void *k_codes, const void *k_scales, const void *v_codes,
                           const void *v_scales, int cache_rows, const void *k_tree, const void *v_tree,
                           const uint64_t *ancestor_mask, const int32_t *kv_start, const int32_t *kv_len,

@@ -40,6 +40,7 @@ _SIGNATURES = {
     "ddtree_sample": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "ddtree_accept_filtered": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz,
                                     _vp]),
+    "ddtree_verify_attn_q4_workspace_bytes": (_sz, [_i] * 6 + [ctypes.c_longlong]),
     "ddtree_verify_attn_q4": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i,
                                    ctypes.c_float, _i, _vp, _vp, _sz, _vp]),
     "ddtree_set_build_algorithm": (_i, [_i]),
@@ -467,6 +468,11 @@ def q4_load(cache, src_row, dst_offset, dtype=torch.bfloat16, out=None, defer=Fa
     args = (*cache.ptrs, cache.rows, src_p, off_p, batch, cache.Hkv, cache.D, code, _ptr(k), _ptr(v), _stream())
     run = _call("ddtree_q4_load", args, out, defer)
     return _keepalive(run, src, off) if defer else run
+
+
+def verify_attn_q4_workspace_bytes(batch, T, Hq, Hkv, D, dtype, sum_L):
+    """Scratch that one verify_attn_q4 call uses for this shape and total cache length."""
+    return int(load().ddtree_verify_attn_q4_workspace_bytes(batch, T, Hq, Hkv, D, dtype, int(sum_L)))
 
 
 def verify_attn_q4(q, cache, k_tree, v_tree, ancestor_mask, kv_start, kv_len, batch, T, Hq, Hkv, D, softmax_scale, dtype, ws,

@@ -71,7 +71,17 @@ extern "C" size_t ddtree_verify_attn_workspace_bytes(int batch, int T, int Hq, i
     if (batch < 1 || batch > DDTREE_MAX_BATCH || T < 1 || T > DDTREE_MAX_N + 1 || Hq < 1 || Hkv < 1 ||
         Hq % Hkv != 0 || D < 8 || D > 256 || D % 8 != 0 || sum_L < 0)
         return 0;
-    return attn_scratch_bytes(batch, T, Hq, Hkv, D, dtype, sum_L);
+    return attn_scratch_bytes(batch, T, Hq, Hkv, D, dtype, sum_L, false);
+}
+
+extern "C" size_t ddtree_verify_attn_q4_workspace_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype,
+                                                        long long sum_L)
+{
+    using namespace ddt;
+    if (batch < 1 || batch > DDTREE_MAX_BATCH || T < 1 || T > DDTREE_MAX_N + 1 || Hq < 1 || Hkv < 1 ||
+        Hq % Hkv != 0 || D < 32 || D > 256 || D % 32 != 0 || sum_L < 0)
+        return 0;
+    return attn_scratch_bytes(batch, T, Hq, Hkv, D, dtype, sum_L, true);
 }
 
 extern "C" int ddtree_profile_enable(unsigned kernel_mask, int capacity)

@@ -1093,8 +1093,8 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
         if (!attn_rows_fit(T, Hq, Hkv)) return DDTREE_ERR_ARG;
         const bool ws_usable = workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0;
         const size_t scratch = ws_usable ? workspace_bytes : 0;
-        if (attn_lacks_scratch(batch, T, Hq, Hkv, D, kv_len, scratch)) return DDTREE_ERR_WORKSPACE;
-        const AttnPlan p = attn_plan(batch, T, Hq, Hkv, D, kv_len, scratch);
+        if (attn_lacks_scratch(batch, T, Hq, Hkv, D, kv_len, scratch, c4 != nullptr)) return DDTREE_ERR_WORKSPACE;
+        const AttnPlan p = attn_plan(batch, T, Hq, Hkv, D, kv_len, scratch, c4 != nullptr);
         if (!ws_ok(workspace, workspace_bytes, p.bytes)) return DDTREE_ERR_WORKSPACE;
         char *wsb = static_cast<char *>(workspace);
         void *part = wsb + p.part_off;

@@ -52,11 +52,11 @@ struct AttnPlan {
 };
 bool attn_mfma_shape(int dtype, int D, int Hkv);
 bool attn_rows_fit(int T, int Hq, int Hkv);  // the query rows of a KV head are counted in 32 bits
-// scratch: bytes at hand.
-AttnPlan attn_plan(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch);
+// scratch: bytes at hand; q4: the cache holds 4-bit codes.
+AttnPlan attn_plan(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch, bool q4);
 bool q4_cache_ok(const void *k_codes, const void *k_scales, const void *v_codes, const void *v_scales, int cache_rows,
                  int Hkv, int D);
-bool attn_lacks_scratch(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch);
+bool attn_lacks_scratch(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch, bool q4);
 
 // ---- attn_wave_kernel ----
 struct AttnWaveSeq {

@@ -140,7 +140,7 @@ struct DivUp {
 // attn_wave_kernel: every sequence's key range in pieces of about the same length, so that the pieces
 // of a ragged batch end together.
 static AttnPlan plan_wave(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, const Lens &lens, int row_blocks, bool wide,
-                          long long room)
+                          long long room, bool q4)
 {
     AttnPlan p{};
     const int M = T * (Hq / Hkv);
@@ -153,16 +153,18 @@ static AttnPlan plan_wave(int batch, int T, int Hq, int Hkv, int D, const int32_
     for (int i = 0; i < lens.n; ++i) sub_tiles += (long long)(lens.sub[i] + tree) * lens.count[i];
     const int nt_max = lens.sub[0] + tree;
     Sized sized[DDTREE_MAX_BATCH];
+    const double value_bytes = q4 ? 1.0625 : 4.0;  // of a key's and a value's element
     // Measured (us): a workgroup's fixed cost (launch, first requests, combining the waves' results), a
     // step of its eight waves (32 keys each), the rates at which the L2s and HBM serve all of them.
     // A step whose keys no L2 holds waits for HBM, in one workgroup's row group at least (48 workgroups of one row
-    // group over 85 MB: 2.7 us; 192 to 512 of four over 79 to 363 MB: 2.3 to 2.5, of ten and more 1.3 to 1.8).
-    const double far = D == 64 ? 0.0 : std::min(1.0, std::max(0.0, ((double)sub_tiles * Hkv * (kSK * 4.0 * D) * 1e-6 - 24.0) / 48.0)) *
+    // group over 85 MB: 2.7 us; 192 to 512 of four over 79 to 363 MB: 2.3 to 2.5, of ten and more 1.3 to 1.8).  Codes of 4 bits:
+    // 1.18 from 16 to 64 steps, alone and with 285 MB of them at work (5.0 TB/s).
+    const double far = D == 64 || q4 ? 0.0 : std::min(1.0, std::max(0.0, ((double)sub_tiles * Hkv * (kSK * value_bytes * D) * 1e-6 - 24.0) / 48.0)) *
                                            (p.groups <= 6 ? 1.0 : p.groups <= 9 ? 0.7 : 0.3);
     const double fix = 7.0, step = D == 64 ? (row_blocks == 1 ? 0.62 : 1.17) : 1.2 + 1.2 * far;
     const double masked = D == 64 ? 0.0 : 0.19;  // more for each sub-tile of a large tree (997 nodes over 230 keys: 2.7 us a step)
-    const double l2_us = (double)sub_tiles * Hkv * p.groups * (kSK * 4.0 * D) / 20.0e6;
-    const double hbm_us = (double)sub_tiles * Hkv * (kSK * 4.0 * D) / 4.0e6;
+    const double l2_us = (double)sub_tiles * Hkv * p.groups * (kSK * value_bytes * D) / 20.0e6;
+    const double hbm_us = (double)sub_tiles * Hkv * (kSK * value_bytes * D) / (q4 ? 5.0e6 : 4.0e6);
     const double least = 5.0 + std::max(l2_us, hbm_us);
     int best_c = nt_max;
     p.cost = 1e30;
@@ -199,7 +201,7 @@ static AttnPlan plan_wave(int batch, int T, int Hq, int Hkv, int D, const int32_
 // attn_mfma_kernel.  Even form: row tiles of the same height.  Uneven form, where the blocks of 32 rows are
 // a few more than whole tiles of 8 (T = 257 with four heads per KV head: 33 blocks): whole tiles, and each
 // block left as a work item of its own with key ranges of its own (attn_wave_rows).
-static AttnPlan plan_main(int batch, int T, int Hq, int Hkv, const int32_t *kv_len, const Lens &lens, bool wide, long long room)
+static AttnPlan plan_main(int batch, int T, int Hq, int Hkv, const int32_t *kv_len, const Lens &lens, bool wide, long long room, bool q4)
 {
     const int nblk = up(T * (Hq / Hkv), 32), full = nblk / 8, rem = nblk % 8;
     const int tree = up(T, kKT), tree_sub = up(T, kSK);
@@ -209,7 +211,7 @@ static AttnPlan plan_main(int batch, int T, int Hq, int Hkv, const int32_t *kv_l
     Sized sized[DDTREE_MAX_BATCH];
     long long key_tiles = 0;
     for (int i = 0; i < lens.n; ++i) key_tiles += (long long)(up(lens.sub[i], 2) + tree) * lens.count[i];
-    const double hbm_us = (double)key_tiles * Hkv * (kKT * 4.0 * kHD) / 5.8e6;
+    const double hbm_us = (double)key_tiles * Hkv * (kKT * (q4 ? 1.0625 : 4.0) * kHD) / 5.8e6;
     // Measured (us): a workgroup's fixed cost and a key tile (below three quarters of the compute units at work,
     // and with all of them, where the chip lowers its clock: 1.92 over 131 key tiles); for a tail block, and a
     // step of eight sub-tiles beside them (1.2 alone, keys from the L2).  With 513 nodes x 32768 keys, four key
@@ -327,29 +329,29 @@ static AttnPlan plan_main(int batch, int T, int Hq, int Hkv, const int32_t *kv_l
 // 401 x 600 21.8 / 25.7, 257 x 8192 102 / 51, 17 x 8192 17.5 / 20.7; 16 sequences of 10 nodes over up to 26246 keys, 16 and
 // 4 heads, 145 / 103, four of 19 over up to 8468 31 / 36.  Heads of 64: 32-row groups against 64-row
 // groups at 257 x 4096 36.9 / 28.5 (two rounds of workgroups against one), at 65 x 2047 11.5 / 13.0.
-AttnPlan attn_plan(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch)
+AttnPlan attn_plan(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch, bool q4)
 {
     long long sum_L = 0;
     for (int i = 0; i < batch; ++i) sum_L += kv_len[i];
     const bool wide = wide_partials(batch, T, Hq, Hkv, D, sum_L);
     const long long room = slot_room(T, Hq, D, wide, scratch);
     const Lens lens = lens_of(kv_len, batch);
-    const AttnPlan w = plan_wave(batch, T, Hq, Hkv, D, kv_len, lens, 1, wide, room);
-    const AttnPlan m = D == kHD ? plan_main(batch, T, Hq, Hkv, kv_len, lens, wide, room)
-                                : plan_wave(batch, T, Hq, Hkv, D, kv_len, lens, 2, wide, room);
+    const AttnPlan w = plan_wave(batch, T, Hq, Hkv, D, kv_len, lens, 1, wide, room, q4);
+    const AttnPlan m = D == kHD ? plan_main(batch, T, Hq, Hkv, kv_len, lens, wide, room, q4)
+                                : plan_wave(batch, T, Hq, Hkv, D, kv_len, lens, 2, wide, room, q4);
     return w.cost <= m.cost ? w : m;
 }
 
 // A long key range that few workgroups share is not walked uncut because a workspace is missing: such a call
 // is refused, unless its plan takes no scratch in any case.
-bool attn_lacks_scratch(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch)
+bool attn_lacks_scratch(int batch, int T, int Hq, int Hkv, int D, const int32_t *kv_len, size_t scratch, bool q4)
 {
     const long long tiles = (long long)batch * Hkv * (((long long)T * (Hq / Hkv) + 255) / 256);
     if (D != kHD || tiles > 128) return false;
     long long sum_L = 0;
     for (int i = 0; i < batch; ++i) sum_L += kv_len[i];
     if ((sum_L / batch + T) / kKT < 8 || slot_room(T, Hq, D, false, scratch) >= 2LL * batch) return false;
-    return attn_plan(batch, T, Hq, Hkv, D, kv_len, SIZE_MAX).bytes > scratch;
+    return attn_plan(batch, T, Hq, Hkv, D, kv_len, SIZE_MAX, q4).bytes > scratch;
 }
 
 size_t attn_scratch_upper(int batch, int T, int Hq, int Hkv, int D)
@@ -366,12 +368,12 @@ size_t attn_scratch_upper(int batch, int T, int Hq, int Hkv, int D)
 
 // The lengths of the sequences are not known here: no key range is shorter than two key tiles, and a
 // single sequence takes what the plan for its length takes.
-size_t attn_scratch_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype, long long sum_L)
+size_t attn_scratch_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype, long long sum_L, bool q4)
 {
     if (!attn_mfma_shape(dtype, D, Hkv) || !attn_rows_fit(T, Hq, Hkv)) return 0;
     if (batch == 1 && sum_L <= 0x7FFFFFFF) {
         const int32_t len = (int32_t)sum_L;
-        return attn_plan(1, T, Hq, Hkv, D, &len, SIZE_MAX).bytes;
+        return attn_plan(1, T, Hq, Hkv, D, &len, SIZE_MAX, q4).bytes;
     }
     const long long slots = std::min(slot_cap(batch, T, Hq, Hkv, D), batch + (sum_L + (T + 128LL) * batch) / (2 * kKT));
     AttnPlan p{};
@@ -580,7 +582,7 @@ static int check_items(const Shape &sh, const AttnPlan &p, std::vector<Item> &it
 }
 
 // kind 0, 1: attn_wave_kernel with 32 and 64 rows; 2: attn_mfma_kernel
-static int check_plan(const Shape &sh, int kind, long long room)
+static int check_plan(const Shape &sh, int kind, long long room, bool q4)
 {
     std::vector<int32_t> kv_start(sh.batch);
     int32_t sum = 0;
@@ -590,17 +592,17 @@ static int check_plan(const Shape &sh, int kind, long long room)
     }
     // the scratch that the library says a call uses is enough for the plan that unlimited scratch gives
     {
-        const AttnPlan free = attn_plan(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), SIZE_MAX);
-        const size_t said = attn_scratch_bytes(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, DDTREE_DTYPE_BF16, sum);
+        const AttnPlan free = attn_plan(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), SIZE_MAX, q4);
+        const size_t said = attn_scratch_bytes(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, DDTREE_DTYPE_BF16, sum, q4);
         if (free.bytes > said || (sh.batch == 1 && free.bytes != said)) return 12;
-        const AttnPlan again = attn_plan(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), said);
+        const AttnPlan again = attn_plan(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), said, q4);
         if (again.bytes != free.bytes || again.items != free.items || again.cost != free.cost) return 13;
-        if (attn_lacks_scratch(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), said)) return 14;
+        if (attn_lacks_scratch(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), said, q4)) return 14;
     }
     const bool wide = wide_partials(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sum);
     const Lens lens = lens_of(sh.len.data(), sh.batch);
-    const AttnPlan p = kind == 2 ? plan_main(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.len.data(), lens, wide, room)
-                                 : plan_wave(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), lens, kind + 1, wide, room);
+    const AttnPlan p = kind == 2 ? plan_main(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.len.data(), lens, wide, room, q4)
+                                 : plan_wave(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D, sh.len.data(), lens, kind + 1, wide, room, q4);
     if (p.slots > room || p.bytes > attn_scratch_upper(sh.batch, sh.T, sh.Hq, sh.Hkv, sh.D)) return 1;
     std::vector<Item> items;
     if (kind == 2) {
@@ -660,7 +662,8 @@ int attn_selftest_host()
         for (int kind = 0; kind < 3; ++kind)
             for (long long room : {1ll << 40, 0ll}) {  // with scratch and without
                 if ((kind == 1 && sh.D != 64) || (kind == 2 && sh.D != kHD)) continue;
-                if (const int rc = check_plan(sh, kind, room)) return 100 * si + rc;
+                for (int q4 = 0; q4 < 2; ++q4)
+                if (const int rc = check_plan(sh, kind, room, q4 != 0)) return 100 * si + rc;
             }
     }
     uint64_t seed = 1;
@@ -682,7 +685,8 @@ int attn_selftest_host()
         const long long room = below(3) == 0 ? below(4 * sh.batch) : 1ll << 40;
         for (int kind = 0; kind < 3; ++kind) {
             if ((kind == 1 && sh.D != 64) || (kind == 2 && sh.D != kHD)) continue;
-            if (const int rc = check_plan(sh, kind, room)) return 100 * si + rc;
+            for (int q4 = 0; q4 < 2; ++q4)
+                if (const int rc = check_plan(sh, kind, room, q4 != 0)) return 100 * si + rc;
         }
     }
     return 0;

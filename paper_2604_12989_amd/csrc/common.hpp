@@ -55,7 +55,7 @@ size_t topk_scratch_upper(int batch, int B, int V, int K);
 
 // ---- attention scratch (bytes): what ddtree_verify_attn may use for a shape and total cache length,
 //      and for any cache length ----
-size_t attn_scratch_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype, long long sum_L);
+size_t attn_scratch_bytes(int batch, int T, int Hq, int Hkv, int D, int dtype, long long sum_L, bool q4);
 size_t attn_scratch_upper(int batch, int T, int Hq, int Hkv, int D);
 
 // ---- layout of the accept scratch ----

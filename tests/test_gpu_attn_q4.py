@@ -159,7 +159,7 @@ def test_rows_of_the_largest_cache_offsets():
 def test_a_workspace_of_the_advertised_size_is_enough(T, lens, Hq, Hkv, D):
     import paper_2604_12989_amd as dd
     c = Case(T, T, lens, Hq, Hkv, D)
-    need = dd.verify_attn_workspace_bytes(1, T, Hq, Hkv, D, dd.DTYPE_BF16, lens[0])
+    need = dd.verify_attn_q4_workspace_bytes(1, T, Hq, Hkv, D, dd.DTYPE_BF16, lens[0])
     full = c.run()
     assert torch.equal(c.run(scratch=need), full)
     c.check(full)
