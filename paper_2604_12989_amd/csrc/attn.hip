@@ -229,7 +229,7 @@ __device__ __forceinline__ void attn_mfma_body(
                                              (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
         };
         if (dma_rank < 0) return;
-        if (valid_ == kKT) {
+        if (!Q4 && valid_ == kKT) {  // (Q4: the offsets are worked out again for the few tiles of the tree, and not held)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 dma(kp, k_src[i], st + (n_dma * i + dma_rank) * 1024);
@@ -267,10 +267,9 @@ __device__ __forceinline__ void attn_mfma_body(
 
     // Everything in LDS is addressed from a 256-byte boundary: the V operand addresses below take
     // an exclusive-or on bits 6 and 7.
-    // Q4: the block that this thread brings of a cache tile, of key q4_row its elements 32 q4_blk on.  K goes to the padded
+    // Q4: the block that a thread brings of a cache tile: of key (t & 255) / 4 its elements 32 (t & 3) on.  K goes to the padded
     // rows; of V's 64-byte blocks, at block ^ (row & 3) as everywhere, the four chunks sit at chunk ^ (row & 3), so that the
     // 16 lanes that write chunk c of four rows' blocks do not meet on a bank.
-    const uint32_t q4_tid = (uint32_t)tid & 255u;
     const bool q4_v = Q4 && wave_u >= kWaves / 2;
     const uint8_t *q4_codes = nullptr, *q4_scales = nullptr;
     u32x4 q4_code = (u32x4){0u, 0u, 0u, 0u};
@@ -282,8 +281,11 @@ __device__ __forceinline__ void attn_mfma_body(
     }
     auto q4_fetch = [&](int tt) __attribute__((always_inline)) {
         const uint64_t key = (uint64_t)(uint32_t)tt * kKT;
-        const uint32_t r = min((int)(q4_tid >> 2), L - 1 - (int)key);  // (rows past the end repeat the last)
-        const uint32_t at = r * 4 + (q4_tid & 3);
+        int t = (int)threadIdx.x;
+        asm volatile("" : "+v"(t));
+        uint32_t at = (uint32_t)t & 255u;
+        const int last = L - 1 - (int)key;
+        if (last < kKT - 1) at = min((int)(at >> 2), last) * 4 + (at & 3u);  // (rows past the end repeat the last)
         q4_code = *reinterpret_cast<const u32x4 *>(q4_codes + key * (kHD / 2) + at * 16);
         q4_scale = q4_scales[key * (kHD / 32) + at];
     };

@@ -158,10 +158,10 @@ static AttnPlan plan_wave(int batch, int T, int Hq, int Hkv, int D, const int32_
     // step of its eight waves (32 keys each), the rates at which the L2s and HBM serve all of them.
     // A step whose keys no L2 holds waits for HBM, in one workgroup's row group at least (48 workgroups of one row
     // group over 85 MB: 2.7 us; 192 to 512 of four over 79 to 363 MB: 2.3 to 2.5, of ten and more 1.3 to 1.8).  Codes of 4 bits:
-    // 1.18 from 16 to 64 steps, alone and with 285 MB of them at work (5.0 TB/s).
+    // 1.18 from 16 to 64 steps where few compute units work, and with 285 MB of them (5.0 TB/s); 1.34 with all at work.
     const double far = D == 64 || q4 ? 0.0 : std::min(1.0, std::max(0.0, ((double)sub_tiles * Hkv * (kSK * value_bytes * D) * 1e-6 - 24.0) / 48.0)) *
                                            (p.groups <= 6 ? 1.0 : p.groups <= 9 ? 0.7 : 0.3);
-    const double fix = 7.0, step = D == 64 ? (row_blocks == 1 ? 0.62 : 1.17) : 1.2 + 1.2 * far;
+    const double fix = 7.0, step = D == 64 ? (row_blocks == 1 ? 0.62 : 1.17) : q4 ? 1.34 : 1.2 + 1.2 * far;
     const double masked = D == 64 ? 0.0 : 0.19;  // more for each sub-tile of a large tree (997 nodes over 230 keys: 2.7 us a step)
     const double l2_us = (double)sub_tiles * Hkv * p.groups * (kSK * value_bytes * D) / 20.0e6;
     const double hbm_us = (double)sub_tiles * Hkv * (kSK * value_bytes * D) / (q4 ? 5.0e6 : 4.0e6);
