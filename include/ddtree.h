@@ -321,7 +321,8 @@ int ddtree_q4_load(const void *k_codes, const void *k_scales, const void *v_code
 /*
  * ddtree_verify_attn_spans over a 4-bit cache: sequence s owns its rows kv_start[s] .. kv_start[s] + kv_len[s] - 1
  * (below cache_rows), whose keys and values are what the codes stand for; the tree rows are tensors of dtype, as there.
- * T = 1 with the one bit of the mask set is a plain decoding step: the token sees the cache and itself.
+ * T = 1 with the one bit of the mask set is a plain decoding step: the token sees the cache and itself.  Rows of a span must
+ * hold finite values (no byte of 255 among their scales); rows of the cache outside the spans are not read.
  * Arguments otherwise, precision and workspace as in ddtree_verify_attn (its own size for one shape:
  * ddtree_verify_attn_q4_workspace_bytes, as ddtree_verify_attn_workspace_bytes is for that call); D a multiple of 32.
  */

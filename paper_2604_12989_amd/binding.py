@@ -160,9 +160,13 @@ def _host_i32(values, n, what):
         values = np.ascontiguousarray(np.asarray(values, dtype=np.int32))
     if values.shape != (n,):
         raise DDTreeError(what)
-    if n > 0 and values.flags.writeable:
-        return values, ctypes.addressof(ctypes.c_char.from_buffer(values))
-    return values, values.ctypes.data
+    return values, _address(values)
+
+
+def _address(values):
+    if values.size > 0 and values.flags.writeable:
+        return ctypes.addressof(ctypes.c_char.from_buffer(values))
+    return values.ctypes.data
 
 
 def workspace_bytes(batch, B, V, N, Hq, Hkv, D, max_sum_L) -> int:
@@ -327,7 +331,7 @@ def _options(batch, temperature, top_k, top_p, min_p):
         return v
     arrays = (one(temperature, np.float32, "temperature"), one(top_k, np.int32, "top_k"), one(top_p, np.float32, "top_p"),
               one(min_p, np.float32, "min_p"))
-    return arrays, tuple(a.ctypes.data for a in arrays)
+    return arrays, tuple(_address(a) for a in arrays)
 
 
 def sample(logits, uniforms, ws, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, defer=False):
@@ -338,9 +342,12 @@ def sample(logits, uniforms, ws, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
     if logits.dim() not in (2, 3) or uniforms.numel() * logits.shape[-1] != logits.numel():
         raise DDTreeError("logits must be [batch, T, V] or [batch, V], with one uniform a row")
     batch, T, V = logits.shape if logits.dim() == 3 else (logits.shape[0], 1, logits.shape[1])
-    _current(logits.get_device())
     if out is None:
         out = torch.empty_like(uniforms, dtype=torch.int32)
+    _dev(out, torch.int32, "out")
+    if out.numel() != batch * T or len({t.get_device() for t in (logits, uniforms, out)}) != 1:
+        raise DDTreeError("out: expected an entry a row, all tensors on one device")
+    _current(logits.get_device())
     arrays, ptrs = _options(batch, temperature, top_k, top_p, min_p)
     p, n = _ws(ws)
     args = (_ptr(logits), batch, T, V, *ptrs, _ptr(uniforms), _ptr(out), p, n, _stream())
@@ -354,12 +361,12 @@ def accept_filtered(target_logits, tokens, parent, depth, n_nodes, B, uniforms, 
     _dev(target_logits, torch.float32, "target_logits")
     _dev(uniforms, torch.float32, "uniforms")
     batch, T, V = target_logits.shape
-    if uniforms.numel() != batch * T:
-        raise DDTreeError("uniforms must be [batch, T]")
+    if uniforms.numel() != batch * T or uniforms.get_device() != target_logits.get_device():
+        raise DDTreeError("uniforms must be [batch, T], on the device of target_logits")
     for name, t, count in (("tokens", tokens, batch * T), ("parent", parent, batch * T), ("depth", depth, batch * T), ("n_nodes", n_nodes, batch)):
         _dev(t, torch.int32, name)
-        if t.numel() != count:
-            raise DDTreeError(f"{name}: expected {count} entries")
+        if t.numel() != count or t.get_device() != target_logits.get_device():
+            raise DDTreeError(f"{name}: expected {count} entries on the device of target_logits")
     _current(target_logits.get_device())
     if out is None:
         n_accepted = torch.empty_like(n_nodes)
@@ -396,6 +403,7 @@ class CacheQ4:
             raise DDTreeError("the tensors of a cache are on one device")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.Hkv, self.rows, self.D, self.device = Hkv, rows, 2 * half, k_codes.get_device()
+        self.row = torch.Size((Hkv, 2 * half))  # of a tensor of keys or values
         self.ptrs = (_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
 
     @classmethod
@@ -411,8 +419,7 @@ _ROW_DTYPE = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32}
 def _rows(t, cache, what):
     """A tensor of K or V rows that goes with the cache; its DTYPE_*."""
     dtype = _ROW_DTYPE.get(t.dtype) if isinstance(t, torch.Tensor) else None
-    if dtype is None or not t.is_cuda or not t.is_contiguous() or t.dim() != 3 or t.shape[1] != cache.Hkv or \
-            t.shape[2] != cache.D or t.get_device() != cache.device:
+    if dtype is None or not t.is_cuda or t.shape[1:] != cache.row or not t.is_contiguous() or t.get_device() != cache.device:
         raise DDTreeError(f"{what}: expected a contiguous bfloat16 or float32 tensor [rows, {cache.Hkv}, {cache.D}] on the cache's device")
     _current(cache.device)
     return dtype
@@ -459,7 +466,7 @@ def q4_load(cache, src_row, dst_offset, dtype=torch.bfloat16, out=None, defer=Fa
     if out is None:
         if dtype not in _ROW_DTYPE:
             raise DDTreeError("dtype: expected torch.bfloat16 or torch.float32")
-        k = torch.empty((int(off[-1]), cache.Hkv, cache.D), dtype=dtype, device=cache.k_codes.device)
+        k = cache.k_codes.new_empty((int(off[-1]), cache.Hkv, cache.D), dtype=dtype)
         out = k, torch.empty_like(k)
     k, v = out
     code = _rows(k, cache, "k")
@@ -485,13 +492,15 @@ def verify_attn_q4(q, cache, k_tree, v_tree, ancestor_mask, kv_start, kv_len, ba
         if t.numel() != batch * T * heads * D or t.get_device() != cache.device:
             raise DDTreeError(f"{name}: expected [batch*T, {heads}, {D}] on the cache's device")
     _dev(ancestor_mask, torch.int64, "ancestor_mask")
-    if ancestor_mask.numel() != batch * T * ((T + 63) // 64):
-        raise DDTreeError("ancestor_mask must be [batch, T, ceil(T/64)]")
+    if ancestor_mask.numel() != batch * T * ((T + 63) // 64) or ancestor_mask.get_device() != cache.device:
+        raise DDTreeError("ancestor_mask must be [batch, T, ceil(T/64)], on the cache's device")
     _current(cache.device)
     start, start_p = _host_i32(kv_start, batch, "kv_start and kv_len must have batch entries each")
     length, length_p = _host_i32(kv_len, batch, "kv_start and kv_len must have batch entries each")
     if out is None:
         out = torch.empty_like(q)
+    elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != cache.device:
+        raise DDTreeError("out: expected a contiguous tensor like q")
     p, n = _ws(ws)
     args = (_ptr(q), *cache.ptrs, cache.rows, _ptr(k_tree), _ptr(v_tree), _ptr(ancestor_mask), start_p, length_p, batch, T,
             Hq, Hkv, D, softmax_scale, dtype, _ptr(out), p, n, _stream())

@@ -78,8 +78,31 @@ struct StepSum {
     ArgPart mass, count;
 };
 
-// Segments of 6144 elements, 24 a thread; of 2048 where those make
-// fewer than two workgroups a compute unit.  The lists together hold about 1400 of a row's largest, enough for the usual top-k.
+// How many of its largest elements a segment lists, and the room for them (the number that reach the bound varies).  The
+// lists together hold about 1400 of a row's largest, enough for the usual top-k.
+static int list_size(int segs) { return std::min(200, std::max(16, 1400 / segs)); }
+static int list_room(int segs)
+{
+    int room = 64;
+    while (5 * room < 8 * list_size(segs)) room *= 2;
+    return room;
+}
+static void sample_layout(SamplePlan &p, long long rows, int V)
+{
+    p.hot = list_size(p.segs);
+    p.hot_cap = list_room(p.segs);
+    p.parts = (V + kPart - 1) / kPart;
+    p.slots = (int)std::min<long long>(rows, kSlots);
+    const size_t per = (size_t)rows * p.segs;
+    p.stat_off = 0;
+    p.hot_off = align_up(per * sizeof(SegStat), 256);
+    p.part_off = p.hot_off + align_up(per * p.hot_cap * 8, 256);
+    p.hard_off = p.part_off + align_up((size_t)rows * 8, 256);
+    p.step_off = p.hard_off + align_up(256 + (size_t)rows * sizeof(HardRow), 256);
+    p.bytes = p.step_off + align_up((size_t)p.slots * p.parts * ((kSteps + 1) * sizeof(StepSum)), 256);
+}
+
+// Segments of 6144 elements, 24 a thread; of 2048 where those make fewer than two workgroups a compute unit.
 static SamplePlan sample_plan(int batch, int T, int V)
 {
     SamplePlan p{};
@@ -87,34 +110,26 @@ static SamplePlan sample_plan(int batch, int T, int V)
     p.vecs = rows * ((V + 6143) / 6144) < 512 && V <= 2048ll * kMaxSegs ? 2 : 6;
     p.seg_len = p.vecs * 1024;
     p.segs = (V + p.seg_len - 1) / p.seg_len;
-    p.hot = std::min(200, std::max(16, 1400 / p.segs));
-    p.hot_cap = 64;
-    while (p.hot_cap < 2 * p.hot) p.hot_cap *= 2;
-    const size_t per = (size_t)rows * p.segs;
-    p.stat_off = 0;
-    p.hot_off = align_up(per * sizeof(SegStat), 256);
-    p.part_off = p.hot_off + align_up(per * p.hot_cap * 8, 256);
-    p.parts = (V + kPart - 1) / kPart;
-    p.hard_off = p.part_off + align_up((size_t)rows * 8, 256);
-    p.step_off = p.hard_off + align_up(256 + (size_t)rows * sizeof(HardRow), 256);
-    p.slots = (int)std::min<long long>(rows, kSlots);
-    p.bytes = p.step_off + align_up((size_t)p.slots * p.parts * ((kSteps + 1) * sizeof(StepSum)), 256);
+    sample_layout(p, rows, V);
     return p;
 }
 
-// A bound on sample_plan(...).bytes over every call of at most this many rows and elements.
+// A bound on sample_plan(...).bytes over every call of at most this many rows and elements: the largest layout for any
+// number of segments, the short ones with no more rows than leave them short.
 size_t sample_scratch_upper(int batch, int T, int V)
 {
-    const size_t rows = (size_t)batch * T;
+    const long long rows = (long long)batch * T;
     size_t most = 0;
     if (V > kSampleMaxV) V = kSampleMaxV;
-    // (a segment's list is at most four times what 1400 divided by the segments asks for, or 64; short segments only below 512
-    // workgroups of long ones)
-    const size_t long_segs = rows * ((V + 6143) / 6144), short_segs = std::min<size_t>(rows * ((V + 2047) / 2048), 512 * 4 + rows);
-    const size_t segs = std::max(long_segs, short_segs);
-    most = segs * (sizeof(SegStat) + 64 * 8) + rows * (size_t)(4 * 1600) * 8 + rows * (8 + sizeof(HardRow)) + 2048 +
-           std::min<size_t>(rows, kSlots) * ((V + kPart - 1) / kPart) * ((kSteps + 1) * sizeof(StepSum));
-    return align_up(most, 256);
+    for (int vecs : {2, 6})
+        for (int segs = 1; segs <= kMaxSegs && (segs - 1) * (vecs * 1024ll) < V; ++segs) {
+            const long long longs = ((segs - 1) * 2048ll + 1 + 6143) / 6144;  // at least, with `segs` short ones
+            SamplePlan p{};
+            p.segs = segs;
+            sample_layout(p, vecs == 6 ? rows : std::min(rows, std::max(1ll, 511 / longs)), V);
+            most = std::max(most, p.bytes);
+        }
+    return most;
 }
 
 // 2^t for t <= 0: 2^f, f within half of 0, from its interpolation at ten Chebyshev nodes (6e-16 off); 1 at 0 exactly.
@@ -1210,6 +1225,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
             border = at;
             if (!gather(border)) return false;
             floor = last_in_step(false, s.count[border], (double)top_k);
+            if (floor == ~0ull) return false;
             kept = s.mass[border] + weight_from_floor();
         }
     }
@@ -1268,6 +1284,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     wave_last(&sh.n, last >= 0, last);
     __syncthreads();
     const int p = sh.n;
+    if (p < 0) return false;
     const ArgPart base = s.part[p];
     constexpr int kEach = kPart / NT;
     const int id0 = p * kPart + tid * kEach;
@@ -1447,11 +1464,17 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_PICK, st, sample_pick_kernel, dim3(T, batch), dim3(kPickThreads), 0, st, logits, T, V, p.seg_len, p.segs,
                p.hot_cap, n_nodes, uniforms, stat, hot, *part, tokens, n_hard, hard, opt);
     // (a row goes on the list by what its logits are: these look whether there are any)
-    const int rows = batch * T, most = (int)std::min<long long>(kStepGrid, (long long)p.slots * p.parts);
-    DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_STEPS, st, sample_steps_kernel, dim3(most), dim3(kStepThreads), 0, st, logits, T, V, p.parts, p.slots,
-               n_hard, hard, steps, opt);
+    // Rows of a small top-k or without filters are hardly ever on it, and are then read as often as it takes: no launch for
+    // their steps (257 rows of 151936 by top-k 50: 51 -> 48 us).
+    bool shared = false;
+    for (int s = 0; s < batch; ++s)
+        shared = shared || (opt.tau[s] > 0.0f && (opt.top_k[s] > 700 || (opt.top_k[s] == 0 && (opt.top_p[s] < 1.0f || opt.min_p[s] > 0.0f))));
+    const int rows = batch * T, slots = shared ? p.slots : 0, most = (int)std::min<long long>(kStepGrid, (long long)p.slots * p.parts);
+    if (shared)
+        DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_STEPS, st, sample_steps_kernel, dim3(most), dim3(kStepThreads), 0, st, logits, T, V, p.parts,
+                   slots, n_hard, hard, steps, opt);
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_AGAIN, st, sample_again_kernel, dim3(std::min(rows, kAgainGrid)), dim3(kAgainThreads), 0, st, logits, T, V,
-               p.parts, p.slots, uniforms, n_hard, hard, steps, *part, tokens, opt);
+               p.parts, slots, uniforms, n_hard, hard, steps, *part, tokens, opt);
     return launch_status();
 }
 
