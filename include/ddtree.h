@@ -398,8 +398,9 @@ int ddtree_build_handovers(unsigned int *count);
 #define DDTREE_KERNEL_SAMPLE_SCAN 10
 #define DDTREE_KERNEL_SAMPLE_PICK 11
 #define DDTREE_KERNEL_SAMPLE_STEPS 12
-#define DDTREE_KERNEL_SAMPLE_AGAIN 13
-#define DDTREE_KERNEL_COUNT 14
+#define DDTREE_KERNEL_SAMPLE_GATHER 13
+#define DDTREE_KERNEL_SAMPLE_AGAIN 14
+#define DDTREE_KERNEL_COUNT 15
 int ddtree_profile_enable(unsigned kernel_mask, int capacity);
 int ddtree_profile_enable_every(unsigned kernel_mask, int capacity, int every);
 int ddtree_profile_reset(void);

@@ -55,7 +55,8 @@ _SIGNATURES = {
 
 KERNELS = {"topk_chunk": 0, "topk_merge": 1, "build": 2, "attn": 3, "attn_merge": 4,
            "accept_argmax": 5, "accept_walk": 6, "attn_generic": 7, "q4_write": 8, "q4_read": 9,
-           "sample_scan": 10, "sample_pick": 11, "sample_steps": 12, "sample_again": 13}
+           "sample_scan": 10, "sample_pick": 11, "sample_steps": 12, "sample_gather": 13,
+           "sample_again": 14}
 
 
 class DDTreeError(RuntimeError):

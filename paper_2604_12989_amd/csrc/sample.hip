@@ -64,14 +64,16 @@ static_assert(sizeof(SegStat) == 32, "one line of two 16-byte stores");
 struct SamplePlan {
     int segs, seg_len, vecs, hot, hot_cap;  // elements that a list is to hold, and room for
     int parts, slots;  // of a row on the list; rows that the steps' sums have room for
-    size_t stat_off, hot_off, part_off, hard_off, step_off, bytes;
+    size_t stat_off, hot_off, part_off, hard_off, step_off, few_off, bytes;
 };
 
 // A row on the list, and what is known of it.
 struct HardRow {
     double sum, best;   // of its weights (0: not known), its largest logit
     double scale;       // steps of the logit for a log-weight
-    int32_t row, pad;
+    int32_t row;
+    int32_t border, listed;  // the step whose elements were gathered (-1: none yet), their number
+    int32_t pad;
 };
 // In front of each step of the logit, over kPart elements: their weights and their number.
 struct StepSum {
@@ -99,7 +101,8 @@ static void sample_layout(SamplePlan &p, long long rows, int V)
     p.part_off = p.hot_off + align_up(per * p.hot_cap * 8, 256);
     p.hard_off = p.part_off + align_up((size_t)rows * 8, 256);
     p.step_off = p.hard_off + align_up(256 + (size_t)rows * sizeof(HardRow), 256);
-    p.bytes = p.step_off + align_up((size_t)p.slots * p.parts * ((kSteps + 1) * sizeof(StepSum)), 256);
+    p.few_off = p.step_off + align_up((size_t)p.slots * p.parts * ((kSteps + 1) * sizeof(StepSum)), 256);
+    p.bytes = p.few_off + align_up((size_t)p.slots * kStepList * 8, 256);
 }
 
 // Segments of 6144 elements, 24 a thread; of 2048 where those make fewer than two workgroups a compute unit.
@@ -450,8 +453,12 @@ struct PickRow {
     template <int NT>
     __device__ __forceinline__ void collect(float lo, float hi, ArgPart *list, int room, int *n) const
     {
-        constexpr int kAhead = 8;
-        const Run run(x, V);
+        collect_of<NT, 8>(Run(x, V), 0, lo, hi, list, room, n);
+    }
+    // The same of a run of the row, `start` elements into it.
+    template <int NT, int kAhead>
+    __device__ __forceinline__ void collect_of(const Run &run, int start, float lo, float hi, ArgPart *list, int room, int *n) const
+    {
         const int lane = threadIdx.x & 63;
         for (int g0 = (int)threadIdx.x - lane; g0 < run.groups; g0 += kAhead * NT) {  // (uniform over a wave)
             float4 p[kAhead];
@@ -477,15 +484,15 @@ struct PickRow {
                     const unsigned long long who = __builtin_amdgcn_ballot_w64(hit);
                     if (who == 0ull) continue;
                     const int mine = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
-                    if (hit && mine < room) list[mine] = arg_part(e[u][v], run.id(g0 + lane + u * NT) + v);
+                    if (hit && mine < room) list[mine] = arg_part(e[u][v], start + run.id(g0 + lane + u * NT) + v);
                     at += __popcll(who);
                 }
         }
         const int edge = run.edge_id();
-        const float v = edge >= 0 ? clean(x[edge]) : -INFINITY;
+        const float v = edge >= 0 ? clean(run.p[edge]) : -INFINITY;
         if (v >= lo && v <= hi) {
             const int mine = atomicAdd(n, 1);
-            if (mine < room) list[mine] = arg_part(v, edge);
+            if (mine < room) list[mine] = arg_part(v, start + edge);
         }
     }
     // A logit whose log-weight is at least t, and whose neighbours' are not far below: what `each` is to look at
@@ -494,6 +501,9 @@ struct PickRow {
         const double v = M + t / c;
         return (float)fmax(-3.4028234e38, fmin(3.4028234e38, v + side * (1e-5 * (fabs(v) + fabs(M)) + 1e-30)));
     }
+    // ends of a step, a little outside
+    __device__ __forceinline__ float lo_of(int step) const { return about(step == kSteps - 1 ? kCut : (step + 1) / scale, -1.0); }
+    __device__ __forceinline__ float hi_of(int step) const { return about(step / scale, 1.0); }
 };
 __device__ __forceinline__ PickRow pick_row(const float *logits, size_t row, int V, double M, float tau)
 {
@@ -667,7 +677,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
         // not make up half of what it leaves out: the steps go that far only
         double deep = -kCut;
         if (sum > 0.0 && top_p < 1.0f) deep = fmin(deep, fmax(1.0, log2((double)V / ((1.0 - (double)top_p) * sum)) + 2.0));
-        hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, -kSteps / deep, (int32_t)row, 0};
+        hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, -kSteps / deep, (int32_t)row, -1, 0, 0};
     };
 
     // The row's sum.  A segment has also counted elements that are too small beside the row's best but not beside its own:
@@ -1120,31 +1130,42 @@ __device__ __forceinline__ double unit_of(double sum, int V)
     return __builtin_amdgcn_ldexp(1.0, 61 - (sum > 0.0 ? __builtin_amdgcn_frexp_exp(sum) : 32 - __builtin_clz((unsigned)V)));
 }
 
-// The last workgroup of a row: the border from the steps' sums, the token.  False: too many elements in the border's step.
+// Weight and count of the thread's step over a row, from its parts' sums (threads past the steps: nothing).
+__device__ __forceinline__ void step_totals(const StepSum *steps, int parts, ArgPart &mass, ArgPart &count)
+{
+    mass = count = 0ull;
+    if (threadIdx.x >= kSteps) return;
+    for (int p = 0; p < parts; p += 8) {
+        StepSum q[16];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            const StepSum *const at = steps + (size_t)min(p + v, parts - 1) * (kSteps + 1) + threadIdx.x;
+            q[2 * v] = at[0], q[2 * v + 1] = at[1];
+        }
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            mass += p + v < parts ? q[2 * v + 1].mass - q[2 * v].mass : 0ull;
+            count += p + v < parts ? q[2 * v + 1].count - q[2 * v].count : 0ull;
+        }
+    }
+}
+__device__ __forceinline__ int step_of_min_p(const PickRow &r, float min_p)
+{
+    return min_p > 0.0f ? r.step_of(fmax(log2((double)min_p), kCut)) : kSteps;
+}
+
+// The border from the steps' sums, then the token.  `few`: the elements of step `ready`, gathered by others.  False: too many elements
+// in the border's step.
 __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts, double unit, int top_k, float top_p, float min_p,
-                              float u, AgainShared &sh, int &token)
+                              float u, int ready, int listed, const ArgPart *few, AgainShared &sh, int &token)
 {
     constexpr int NT = kAgainThreads;
     static_assert(NT >= kSteps, "a thread a step");
     auto &s = sh.s;
     const int tid = threadIdx.x;
     // weight and count of each step over the row, then in front of it
-    ArgPart mass = 0ull, count = 0ull, mass_all, count_all;
-    if (tid < kSteps) {
-        for (int p = 0; p < parts; p += 8) {
-            StepSum q[16];
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                const StepSum *const at = steps + (size_t)min(p + v, parts - 1) * (kSteps + 1) + tid;
-                q[2 * v] = at[0], q[2 * v + 1] = at[1];
-            }
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                mass += p + v < parts ? q[2 * v + 1].mass - q[2 * v].mass : 0ull;
-                count += p + v < parts ? q[2 * v + 1].count - q[2 * v].count : 0ull;
-            }
-        }
-    }
+    ArgPart mass, count, mass_all, count_all;
+    step_totals(steps, parts, mass, count);
     const ArgPart mass_front = block_scan<NT>(mass, sh.wave_u, mass_all), count_front = block_scan<NT>(count, sh.wave_u, count_all);
     if (tid < kSteps) s.mass[tid] = mass_front, s.count[tid] = count_front;
     // Elements of steps in front of `border` stay, those behind it do not; of it those from `floor` on with a weight of min_p.
@@ -1160,13 +1181,20 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         return at;
     };
     auto gather = [&](int step) {  // the step's elements that take part, into s.list, anything else there as 0; false: too many
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        r.collect<NT>(r.about(step == kSteps - 1 ? kCut : (step + 1) / r.scale, -1.0), r.about(step / r.scale, 1.0), s.list, kStepList, &sh.n);
-        __syncthreads();
-        n = sh.n;
-        __syncthreads();
-        if (n > kStepList) return false;
+        if (step == ready) {
+            n = listed;
+            if (n > kStepList) return false;
+            for (int k = tid; k < n; k += NT) s.list[k] = few[k];
+            __syncthreads();
+        } else {
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+            r.collect<NT>(r.lo_of(step), r.hi_of(step), s.list, kStepList, &sh.n);
+            __syncthreads();
+            n = sh.n;
+            __syncthreads();
+            if (n > kStepList) return false;
+        }
         for (int k = tid; k < n; k += NT) {
             const double t = r.log_weight(key_float((uint32_t)(s.list[k] >> 32)));
             if (!(t >= kCut) || r.step_of(t) != step || s.list[k] < floor) s.list[k] = 0ull;
@@ -1217,7 +1245,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         return all;
     };
     // The step where min-p ends is known ahead; what ends behind it needs no closer look.
-    const int min_step = min_p > 0.0f ? r.step_of(fmax(log2((double)min_p), kCut)) : kSteps;
+    const int min_step = step_of_min_p(r, min_p);
     ArgPart kept = mass_all;  // weight of what top-k keeps
     if (top_k > 0 && count_all > (ArgPart)top_k) {
         const int at = last_below(count_front, count > 0ull, (double)top_k);
@@ -1366,11 +1394,55 @@ __global__ __launch_bounds__(kStepThreads) void sample_steps_kernel(
     }
 }
 
+// The elements of the step where a row's border lies, by the workgroups that took its parts: one alone reads a row of 151936 at
+// what its outstanding loads allow, 26 us.  (Top-p behind a top-k: its border is known only when the first one is, and left.)
+__global__ __launch_bounds__(kStepThreads) void sample_gather_kernel(
+    const float *__restrict__ logits, int T, int V, int parts, int slots, const uint32_t *__restrict__ n_hard,
+    HardRow *hard, const StepSum *__restrict__ steps, ArgPart *__restrict__ few, SampleOpts opt)
+{
+    constexpr int NT = kStepThreads;
+    __shared__ ArgPart s_waves[NT / 64], s_list[kStepList];
+    __shared__ int s_border[2], s_n, s_at;
+    const int tid = threadIdx.x;
+    const int items = min((int)*n_hard, slots) * parts;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int h = item / parts, p = item - h * parts;
+        const int row = hard[h].row, seq = row / T, top_k = opt.top_k[seq];
+        const float top_p = opt.top_p[seq], min_p = opt.min_p[seq];
+        if (top_k > 0 && top_p < 1.0f) continue;
+        PickRow r = pick_row(logits, (size_t)row, V, hard[h].best, opt.tau[seq]);
+        r.scale = hard[h].scale;
+        ArgPart mass, count, mass_all, count_all;
+        step_totals(steps + (size_t)h * parts * (kSteps + 1), parts, mass, count);
+        __syncthreads();  // (the shared memory of the item before)
+        if (tid == 0) s_border[0] = s_border[1] = -1, s_n = 0;
+        const ArgPart mass_front = block_scan<NT>(mass, s_waves, mass_all), count_front = block_scan<NT>(count, s_waves, count_all);
+        wave_last(&s_border[0], tid < kSteps && count > 0ull && count_front < (ArgPart)top_k, tid);
+        wave_last(&s_border[1], tid < kSteps && mass > 0ull && (double)mass_front < (double)top_p * (double)mass_all, tid);
+        __syncthreads();
+        int border = step_of_min_p(r, min_p);
+        if (top_k > 0 && count_all > (ArgPart)top_k) border = min(border, s_border[0]);
+        if (top_p < 1.0f) border = min(border, s_border[1]);
+        if (border < 0 || border >= kSteps) continue;
+        const int start = p * kPart;
+        r.collect_of<NT, kPart / (4 * NT)>(Run(r.x + start, min(kPart, V - start)), start, r.lo_of(border), r.hi_of(border), s_list, kStepList, &s_n);
+        __syncthreads();
+        if (tid == 0) {
+            s_at = atomicAdd(&hard[h].listed, s_n);
+            if (p == 0) hard[h].border = border;
+        }
+        __syncthreads();
+        const int at = s_at, n = min(s_n, kStepList - at);
+        for (int k = tid; k < n; k += NT) few[(size_t)h * kStepList + at + k] = s_list[k];
+    }
+}
+
 // Then a workgroup a row.  Rows past `slots` (the room for the steps' sums) and those with thousands of elements in one
 // step are read as often as it takes.
 __global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
     const float *__restrict__ logits, int T, int V, int parts, int slots, const float *__restrict__ uniforms, const uint32_t *__restrict__ n_hard,
-    const HardRow *__restrict__ hard, const StepSum *__restrict__ steps, ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
+    const HardRow *__restrict__ hard, const StepSum *__restrict__ steps, const ArgPart *__restrict__ few,
+    ArgPart *__restrict__ part, int32_t *__restrict__ tokens, SampleOpts opt)
 {
     __shared__ AgainShared sh;
     const int n = (int)*n_hard;
@@ -1383,7 +1455,8 @@ __global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
         int token = -1;
         __syncthreads();  // (the shared memory of the row before)
         if (h >= slots ||
-            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit_of(row.sum, V), top_k, top_p, min_p, u, sh, token))
+            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit_of(row.sum, V), top_k, top_p, min_p, u, row.border,
+                           row.listed, few + (size_t)h * kStepList, sh, token))
             token = pick_alone(r, top_k, top_p, min_p, u, sh);
         put_token(token, (size_t)row.row, part, tokens);
     }
@@ -1403,7 +1476,8 @@ int sample_selftest_host()
                 const size_t per = (size_t)batch * T * p.segs;
                 if (p.hot_off < per * sizeof(SegStat) || p.part_off < p.hot_off + per * p.hot_cap * 8 || p.hard_off < p.part_off + (size_t)batch * T * 8 ||
                     p.step_off < p.hard_off + 256 + (size_t)batch * T * sizeof(HardRow) ||
-                    p.bytes < p.step_off + (size_t)p.slots * p.parts * (kSteps + 1) * sizeof(StepSum) ||
+                    p.few_off < p.step_off + (size_t)p.slots * p.parts * (kSteps + 1) * sizeof(StepSum) ||
+                    p.bytes < p.few_off + (size_t)p.slots * kStepList * 8 || (p.few_off & 255u) ||
                     (long long)p.parts * kPart < V || ((p.hot_off | p.part_off | p.hard_off | p.step_off) & 255u))
                     return 10034;
                 const size_t have = sample_scratch_upper(batch, T, V);
@@ -1458,6 +1532,7 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
     uint32_t *const n_hard = reinterpret_cast<uint32_t *>(ws + p.hard_off);
     HardRow *const hard = reinterpret_cast<HardRow *>(ws + p.hard_off + 256);
     StepSum *const steps = reinterpret_cast<StepSum *>(ws + p.step_off);
+    ArgPart *const few = reinterpret_cast<ArgPart *>(ws + p.few_off);
     auto *scan = p.vecs == 2 ? sample_scan_kernel<2> : sample_scan_kernel<6>;
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_SCAN, st, scan, dim3(p.segs, T, batch), dim3(kScanThreads), 0, st, logits, T, V, p.seg_len, p.segs,
                p.hot, p.hot_cap, n_nodes, stat, hot, n_hard, opt);
@@ -1470,11 +1545,14 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
     for (int s = 0; s < batch; ++s)
         shared = shared || (opt.tau[s] > 0.0f && (opt.top_k[s] > 700 || (opt.top_k[s] == 0 && (opt.top_p[s] < 1.0f || opt.min_p[s] > 0.0f))));
     const int rows = batch * T, slots = shared ? p.slots : 0, most = (int)std::min<long long>(kStepGrid, (long long)p.slots * p.parts);
-    if (shared)
+    if (shared) {
         DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_STEPS, st, sample_steps_kernel, dim3(most), dim3(kStepThreads), 0, st, logits, T, V, p.parts,
                    slots, n_hard, hard, steps, opt);
+        DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_GATHER, st, sample_gather_kernel, dim3(most), dim3(kStepThreads), 0, st, logits, T, V, p.parts,
+                   slots, n_hard, hard, steps, few, opt);
+    }
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_AGAIN, st, sample_again_kernel, dim3(std::min(rows, kAgainGrid)), dim3(kAgainThreads), 0, st, logits, T, V,
-               p.parts, slots, uniforms, n_hard, hard, steps, *part, tokens, opt);
+               p.parts, slots, uniforms, n_hard, hard, steps, few, *part, tokens, opt);
     return launch_status();
 }
 
