@@ -16,10 +16,12 @@
 //          from one more read of the segment.  With filters: what stays is mostly among the listed elements above the
 //          largest of the segments' bounds (about 1200 of a row): their ranks and the weights in front of them from
 //          buckets.  A row of which that does not hold (thousands of tokens stay) is put on a list.
-//   steps, again   what is on the list.  First many workgroups a row: each leaves, for 8192 elements, the weight (and the number) in
-//          front of each of 256 steps of the logit.  Then one: it adds them up, reads the row once more for the elements
-//          of the one step where the border lies, and draws the token.  (In one launch, the last workgroup of a row going on
-//          by itself, the fences between the XCDs' caches took 20 times as long as the work.)
+//   steps, gather, again   what is on the list.  Many workgroups a row: each leaves, for 8192 elements, the weight (and the number) in
+//          front of each of 256 steps of the logit; they add these up and gather the elements of the one step where the
+//          border lies; then one puts those in order and draws the token.  (In one launch, the last workgroup of a row going
+//          on by itself, the fences between the XCDs' caches took 20 times as long as the work.)
+// Measured, 257 rows of 151936, top-k 50: scan 28.8 us (5.4 TB/s), pick 11, the empty list 2; 256 flat rows, top-p 0.95: scan 62
+// (some 25 fp64 operations an element), pick 23, steps 71, gather 82, again 23; one flat row 5.5, 15, 6, 8, 18.
 // Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 62 bits allow):
 // their order does not matter.
 #include <algorithm>
