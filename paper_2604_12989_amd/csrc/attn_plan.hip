@@ -663,7 +663,7 @@ int attn_selftest_host()
             for (long long room : {1ll << 40, 0ll}) {  // with scratch and without
                 if ((kind == 1 && sh.D != 64) || (kind == 2 && sh.D != kHD)) continue;
                 for (int q4 = 0; q4 < 2; ++q4)
-                if (const int rc = check_plan(sh, kind, room, q4 != 0)) return 100 * si + rc;
+                    if (const int rc = check_plan(sh, kind, room, q4 != 0)) return 100 * si + rc;
             }
     }
     uint64_t seed = 1;

@@ -72,6 +72,16 @@ def test_many_rows_take_long_segments():
     _check(x, rng.random((3, 33)), temperature=[0.8, 1.0, 1.2], top_p=[0.9, 0.7, 1.0], min_p=[0.0, 0.2, 0.0])
 
 
+@pytest.mark.parametrize("options", [dict(top_p=0.9), dict(top_k=1500), dict(top_k=1500, top_p=0.7), dict(min_p=0.2),
+                                     dict(top_p=0.95, min_p=0.3, temperature=1.3)])
+def test_more_flat_rows_than_have_room_together(options):
+    """600 rows that their lists do not hold; every third value is the same in all of them."""
+    rng = np.random.default_rng(13)
+    x = _rows(rng, 2, 300, 3001, "flat")
+    x[:, :, ::3] = 0.25
+    _check(x, rng.random((2, 300)), **options)
+
+
 @pytest.mark.parametrize("V", [50, 3000, 70000])
 def test_ties(V):
     """Rows of equal logits and of a few values: ranks and running sums go by the ids."""
