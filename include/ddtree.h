@@ -298,14 +298,14 @@ int ddtree_compact(const void *k_tree, const void *v_tree, const int32_t *path,
  * ddtree_q4_store writes prompts: rows src_offset[s] .. src_offset[s+1] - 1 of k / v become the rows from dst_row[s] on.
  *   k, v        [device] [src_offset[batch], Hkv, D]
  *   src_offset  [host] int32 [batch+1], non-decreasing, src_offset[0] >= 0
- *   dst_row     [host] int32 [batch]; where destinations overlap, either sequence's row may stay
+ *   dst_row     [host] int32 [batch]; no row may be written by two sequences (DDTREE_ERR_ARG)
  */
 int ddtree_q4_store(const void *k, const void *v, const int32_t *src_offset, const int32_t *dst_row,
                     int batch, int Hkv, int D, int dtype, void *k_codes, void *k_scales, void *v_codes,
                     void *v_scales, int cache_rows, void *stream);
 
 /* ddtree_compact into such a cache: for j = 0..n_accepted[s] the row dst_row[s] + j becomes tree row s*T + path[s][j].
- * Rows dst_row[s] .. dst_row[s] + B must exist (DDTREE_ERR_ARG otherwise); entries of path outside 0 .. T-1
+ * Rows dst_row[s] .. dst_row[s] + B must exist and be the sequence's own (DDTREE_ERR_ARG otherwise); entries of path outside 0 .. T-1
  * are passed over. */
 int ddtree_q4_append(const void *k_tree, const void *v_tree, const int32_t *path,
                      const int32_t *n_accepted, const int32_t *dst_row, int batch, int T, int B, int Hkv,

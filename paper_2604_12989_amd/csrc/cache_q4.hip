@@ -188,6 +188,17 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether two sequences would write a row both: its codes could be one's and its scales the other's.
+bool q4_shared_rows(const int32_t *first, const int32_t *rows, int batch)
+{
+    for (int s = 1; s < batch; ++s)
+        for (int t = 0; t < s; ++t)
+            if (rows[s] > 0 && rows[t] > 0 && (long long)first[s] < (long long)first[t] + rows[t] &&
+                (long long)first[t] < (long long)first[s] + rows[s])
+                return true;
+    return false;
+}
+
 // Sequence s has rows offset[s] .. offset[s + 1] of the row tensor and as many from cache_row[s] on of the cache.
 // Returns the most rows of a sequence, or -1; the groups of eight elements of a sequence and head are counted in 31 bits.
 int q4_ranges(const int32_t *offset, const int32_t *cache_row, int batch, int cache_rows, int D, int32_t *row0, int32_t *cache0, int32_t *rows)
@@ -227,7 +238,7 @@ extern "C" int ddtree_q4_store(const void *k, const void *v, const int32_t *src_
     if (dtype != DDTREE_DTYPE_BF16 && dtype != DDTREE_DTYPE_FP32) return DDTREE_ERR_ARG;
     Q4Rows args{};
     const int most = q4_ranges(src_offset, dst_row, batch, cache_rows, D, args.src, args.dst, args.rows);
-    if (most < 0) return DDTREE_ERR_ARG;
+    if (most < 0 || q4_shared_rows(args.dst, args.rows, batch)) return DDTREE_ERR_ARG;
     if (most == 0) return DDTREE_OK;  // (a tensor without rows may have no address)
     if (!k || !v || !aligned16(k) || !aligned16(v)) return DDTREE_ERR_ARG;
     const dim3 grid = q4_grid(most, D / 8, Hkv, batch);
@@ -258,7 +269,9 @@ extern "C" int ddtree_q4_append(const void *k_tree, const void *v_tree, const in
     for (int s = 0; s < batch; ++s) {
         if (dst_row[s] < 0 || (long long)dst_row[s] + B + 1 > cache_rows) return DDTREE_ERR_ARG;
         args.dst[s] = dst_row[s];
+        args.rows[s] = B + 1;  // (at most: the kernel goes by n_accepted)
     }
+    if (q4_shared_rows(args.dst, args.rows, batch)) return DDTREE_ERR_ARG;
     const dim3 grid = q4_grid(B + 1, D / 8, Hkv, batch);
     uint32_t *const kc = static_cast<uint32_t *>(k_codes), *const vc = static_cast<uint32_t *>(v_codes);
     uint8_t *const ks = static_cast<uint8_t *>(k_scales), *const vs = static_cast<uint8_t *>(v_scales);

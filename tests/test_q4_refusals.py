@@ -72,6 +72,15 @@ def test_append_refuses_bad_arguments(lib, p):
         assert rc == ERR_ARG, change
 
 
+def test_rows_of_two_sequences_are_refused(lib, p):
+    """Codes and scales of one row could come from either."""
+    for off, row, rc in [((0, 5, 9), (3, 7), ERR_ARG), ((0, 5, 9), (7, 10), ERR_ARG), ((0, 5, 9), (3, 3), ERR_ARG),
+                         ((0, 0, 0), (3, 3), 0), ((2, 2, 2), (12, 3), 0)]:
+        assert lib.ddtree_q4_store(p, p, _i32(*off), _i32(*row), 2, 2, 64, 0, p, p, p, p, 12, None) == rc, (off, row)
+    for row in [(3, 3, 20), (3, 20, 7), (7, 20, 3), (20, 3, 16)]:
+        assert lib.ddtree_q4_append(p, p, p, p, _i32(*row), 3, 5, 4, 2, 64, 0, p, p, p, p, 25, None) == ERR_ARG, row
+
+
 def test_the_binding_refuses_tensors_that_are_no_cache():
     import torch
     import paper_2604_12989_amd as dd
