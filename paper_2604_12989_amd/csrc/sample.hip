@@ -1499,7 +1499,7 @@ static bool sample_opts(ddt::SampleOpts &o, int batch, const float *temperature,
     if (!temperature) return false;
     for (int s = 0; s < batch; ++s) {
         o.tau[s] = temperature[s];
-        o.top_k[s] = top_k ? top_k[s] : 0;
+        o.top_k[s] = top_k ? std::min(top_k[s], (int32_t)ddt::kSampleMaxV) : 0;  // (no row is longer; the kernels multiply it)
         o.top_p[s] = top_p ? top_p[s] : 1.0f;
         o.min_p[s] = min_p ? min_p[s] : 0.0f;
         // (compared by their bits: the compiler takes a comparison to have no NaN in it)

@@ -64,6 +64,24 @@ def test_full_vocabulary(kind):
         _check(x, rng.random((1, 24)), **options)
 
 
+@pytest.mark.parametrize("top_k", [32003, 32004, 1 << 30, (1 << 31) - 1])
+def test_top_k_as_long_as_the_row_and_longer(top_k):
+    rng = np.random.default_rng(14)
+    for kind in ("peaked", "flat"):
+        x, u = _rows(rng, 2, 3, 32003, kind), rng.random((2, 3))
+        for rest in (dict(), dict(top_p=0.9), dict(min_p=0.1)):
+            assert np.array_equal(_check(x, u, top_k=top_k, **rest), _sample(x, u, **rest))
+
+
+@pytest.mark.parametrize("V", [1 << 21, (1 << 21) + 1, 1 << 22])
+def test_largest_vocabularies(V):
+    rng = np.random.default_rng(V)
+    for kind in ("peaked", "flat"):
+        x, u = _rows(rng, 1, 2, V, kind), rng.random((1, 2))
+        for options in (dict(), dict(top_k=50, top_p=0.95), dict(top_p=0.9), dict(top_k=100000), dict(min_p=0.3)):
+            _check(x, u, **options)
+
+
 def test_many_rows_take_long_segments():
     rng = np.random.default_rng(12)
     x = _rows(rng, 3, 33, 50021, "peaked")
