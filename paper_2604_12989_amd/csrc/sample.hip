@@ -161,9 +161,11 @@ __device__ __forceinline__ double exp2_of(double t)
 // What counts as a logit: NaN as -inf (never selected), +inf as the largest finite number.
 __device__ __forceinline__ float clean(float x)
 {
-    // (the median of three is the smaller of the other two where one is no number; in the compiler's own terms there are none)
+    // (The median of three is the smaller of the other two where one is no number; in the compiler's own terms there are none.  A
+    // signalling NaN would be made a quiet one inside it, by its first minimum, and be left out of the second, with the largest
+    // finite number as the result: the maximum of x with itself makes it quiet before.)
     float y;
-    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "v"(-INFINITY), "v"(3.4028235e38f));
+    asm("v_max_f32 %0, %1, %1\n\tv_med3_f32 %0, %0, %2, %3" : "=&v"(y) : "v"(x), "v"(-INFINITY), "v"(3.4028235e38f));
     return y;
 }
 constexpr uint32_t kKeyOfNone = 0x007FFFFFu;  // float_key(-inf)
