@@ -22,7 +22,7 @@
 //          on by itself, the fences between the XCDs' caches took 20 times as long as the work.)
 // Measured, 257 rows of 151936, top-k 50: scan 28.8 us (5.4 TB/s), pick 11, the empty list 2; 256 flat rows, top-p 0.95: scan 62
 // (some 25 fp64 operations an element), pick 23, steps 71, gather 82, again 23; one flat row 5.5, 15, 6, 8, 18.
-// Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 62 bits allow):
+// Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 63 bits allow):
 // their order does not matter.
 #include <algorithm>
 
@@ -55,7 +55,7 @@ struct SampleOpts {
 
 struct SegStat {
     ArgPart best;
-    double sum;      // of the weights relative to the segment's best
+    double sum;      // of the weights relative to the segment's best; where the row's sum is not asked for, a bound on it
     float low;       // the smallest element with a weight
     uint32_t bound;  // key: every element that reaches it is listed (0: every finite one)
     int32_t listed;  // more than the list holds: it is not complete
@@ -71,7 +71,7 @@ struct SamplePlan {
 
 // A row on the list, and what is known of it.
 struct HardRow {
-    double sum, best;   // of its weights (0: not known), its largest logit
+    double unit, best;  // units of its integer weights, its largest logit
     double scale;       // steps of the logit for a log-weight
     int32_t row;
     int32_t border, listed;  // the step whose elements were gathered (-1: none yet), their number
@@ -199,6 +199,17 @@ struct Run {
     }
 };
 
+// Sum over the wave; valid in lane 63 only.
+__device__ __forceinline__ float wave_sum_f32_lane63(float v)
+{
+    v += dpp_f<0xB1>(0.0f, v);
+    v += dpp_f<0x4E>(0.0f, v);
+    v += dpp_f<0x141>(0.0f, v);
+    v += dpp_f<0x140>(0.0f, v);
+    v += dpp_f<0x142, 0xA>(0.0f, v);
+    return v + dpp_f<0x143, 0xC>(0.0f, v);
+}
+
 template <int VECS>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
     const float *__restrict__ logits, int T, int V, int seg_len, int segs, int hot_size, int hot_cap,
@@ -282,6 +293,14 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
         low = -wave_max_f32(-low);
         if (lane == 63) s_sum[wave] = sum, s_low[wave] = low;
     }
+    if (filtered && !want_sum && tau > 0.0f && wave == 1) {
+        // (no four threads' elements weigh more than the largest of them each: at most 16 VECS + 4 times the sum, mostly a few times.
+        // Beside the bisection, by a wave that waits for it)
+        const float m = key_float((uint32_t)(best >> 32)), c = fminf(1.44269504f * __builtin_amdgcn_rcpf(tau), 3.4028235e38f);
+        const float top = fmaxf(fmaxf(s_max[lane], s_max[64 + lane]), fmaxf(s_max[128 + lane], s_max[192 + lane]));
+        const float sum = wave_sum_f32_lane63(__builtin_amdgcn_exp2f(fmaxf((top - m) * c, -64.0f)));
+        if (lane == 63) s_sum[0] = (double)(sum * (16 * VECS + 4)), s_sum[1] = s_sum[2] = s_sum[3] = 0.0;
+    }
     if (filtered && tau > 0.0f && wave == 0) {
         // A bound that about `size` elements reach, by bisection over the keys of the thread maxima: as many as
         // 256 (1 - e^(-size / 256)) of these reach a bound that `size` elements at random places do.  Of top-k's tokens a
@@ -348,8 +367,8 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(
         SegStat s{};
         s.best = best;
         s.low = INFINITY;
+        if (tau > 0.0f && best != kNoPart) s.sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
         if (want_sum && best != kNoPart) {
-            s.sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
             s.low = fminf(fminf(s_low[0], s_low[1]), fminf(s_low[2], s_low[3]));
         }
         s.bound = filtered && tau > 0.0f ? s_bound : 0u;
@@ -547,6 +566,10 @@ __device__ __forceinline__ float clean_uniform(float u)
     const uint32_t b = __float_as_uint(u);
     return b > 0x7F800000u ? 0.0f : b >= 0x3F800000u ? 0x1.fffffep-1f : u;
 }
+// Units of the integer weights of a row whose sum is at most `most` (at least 1): as fine as sums below 2^63 allow.  (A bound 100 times
+// the sum leaves a weight off by 2^-56 of it.  By the number of elements alone it was 2^-45 where one token has most of the weight, and with
+// equal others, all rounded alike, borders were off by 1e-9 of the sum.)
+__device__ __forceinline__ double unit_of(double most) { return __builtin_amdgcn_ldexp(1.0, 63 - __builtin_amdgcn_frexp_exp(most)); }
 __device__ __forceinline__ void put_token(int token, size_t row, ArgPart *part, int32_t *tokens)
 {
     if (threadIdx.x != 0) return;
@@ -676,12 +699,23 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
     const bool has_sum = top_k == 0 && (top_p < 1.0f || !filtered);
     double Z = 0.0;
     auto put_on_list = [&](double sum) {
-        if (tid != 0) return;
+        if (tid >= 64) return;
+        // the sum, or a bound on it from those of the segments: the units go by it
+        double most = Z;
+        if (!has_sum) {
+            most = 0.0;
+            for (int s = tid; s < segs; s += 64) {
+                const ArgPart b = stat[s].best;
+                most += b != kNoPart ? exp2_of(r.log_weight(key_float((uint32_t)(b >> 32)))) * stat[s].sum : 0.0;
+            }
+            most = wave_sum_f64_lane63(most);
+        }
+        if (tid != 63) return;
         // Where the sum is known and top-p is the first filter, its border lies above log-weights of which all V elements would
         // not make up half of what it leaves out: the steps go that far only
         double deep = -kCut;
         if (sum > 0.0 && top_p < 1.0f) deep = fmin(deep, fmax(1.0, log2((double)V / ((1.0 - (double)top_p) * sum)) + 2.0));
-        hard[atomicAdd(n_hard, 1u)] = HardRow{sum, r.M, -kSteps / deep, (int32_t)row, -1, 0, 0};
+        hard[atomicAdd(n_hard, 1u)] = HardRow{unit_of(most), r.M, -kSteps / deep, (int32_t)row, -1, 0, 0};
     };
 
     // The row's sum.  A segment has also counted elements that are too small beside the row's best but not beside its own:
@@ -1086,9 +1120,7 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
         double mine = 0.0;
         r.each<NT>([&](float v, int id) { mine += r.weight(v, id); });
         (void)block_scan<NT>(mine, sh.locate.wave_d, total);
-        // as fine as sums below 2^62 allow
-        const double unit = __builtin_amdgcn_ldexp(1.0, 61 - __builtin_amdgcn_frexp_exp(total));
-        r.floor = pick_threshold<true>(r, (double)top_p * total, unit, sh);
+        r.floor = pick_threshold<true>(r, (double)top_p * total, unit_of(total), sh);
     }
     r.min_w = (double)min_p;
     const int chunks = (r.V + kChunk - 1) / kChunk, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -1126,12 +1158,6 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     __syncthreads();
     double c0, c1;
     return pick_locate<NT>(r, k * kChunk, min(kChunk, r.V - k * kChunk), base, target, sh.locate, c0, c1);
-}
-
-// Units of the integer weights of a row: as fine as sums below 2^62 allow.
-__device__ __forceinline__ double unit_of(double sum, int V)
-{
-    return __builtin_amdgcn_ldexp(1.0, 61 - (sum > 0.0 ? __builtin_amdgcn_frexp_exp(sum) : 32 - __builtin_clz((unsigned)V)));
 }
 
 // Weight and count of the thread's step over a row, from its parts' sums (threads past the steps: nothing).
@@ -1359,7 +1385,7 @@ __global__ __launch_bounds__(kStepThreads) void sample_steps_kernel(
         const HardRow row = hard[h];
         const int seq = row.row / T;
         const bool by_count = opt.top_k[seq] > 0;
-        const double unit = unit_of(row.sum, V);
+        const double unit = row.unit;
         PickRow r = pick_row(logits, (size_t)row.row, V, row.best, opt.tau[seq]);
         r.scale = row.scale;
         const int start = p * kPart;
@@ -1459,7 +1485,7 @@ __global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
         int token = -1;
         __syncthreads();  // (the shared memory of the row before)
         if (h >= slots ||
-            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, unit_of(row.sum, V), top_k, top_p, min_p, u, row.border,
+            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, row.unit, top_k, top_p, min_p, u, row.border,
                            row.listed, few + (size_t)h * kStepList, sh, token))
             token = pick_alone(r, top_k, top_p, min_p, u, sh);
         put_token(token, (size_t)row.row, part, tokens);

@@ -1,0 +1,39 @@
+"""Rows that are read again, with uniforms next to a border: the sums that decide hold to what the definition says."""
+import numpy as np
+import pytest
+import torch
+
+from tests import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+
+
+def _sample(x, u, **options):
+    import paper_2604_12989_amd as dd
+    batch, T, V = x.shape
+    ws = dd.Workspace(batch, 1, V, max(1, T - 1), 1, 1, 64, 0)
+    out = dd.sample(gu.to_dev(x.astype(np.float32)), gu.to_dev(u.astype(np.float32)), ws, **options)
+    torch.cuda.synchronize()
+    return out.cpu().numpy()
+
+
+@pytest.mark.parametrize("options,kept", [(dict(min_p=1e-8), 100000), (dict(top_k=90000), 89999)])
+def test_a_likely_token_and_equal_others(options, kept):
+    """Token 0 has weight 1, `kept` others exp(-d) each.  The uniforms lie 4e-4 to 2e-3 of one such weight (3e-10 of the sum and
+    more) from a border of tokens 1 to 20000, on both sides."""
+    V = 100001
+    d = np.float32(14.0703125)
+    w = np.exp(-np.float64(d))
+    S = 1.0 + kept * w
+    # every float above token 0's share: which token, how far above the border in front of it
+    near = np.arange(int(np.ceil(2.0 ** 24 / S)), int(2.0 ** 24 * (1.0 + 20000 * w) / S)) * 2.0 ** -24
+    place = (near * S - 1.0) / w
+    off = place - np.rint(place)
+    far = np.abs(off)
+    near, place = near[(far > 4e-4) & (far < 2e-3)], place[(far > 4e-4) & (far < 2e-3)]
+    pick = np.random.default_rng(1).choice(near.size, 64, replace=False)
+    u, want = near[pick], 1 + np.floor(place[pick]).astype(np.int32)
+    x = np.full((1, 64, V), -d, np.float32)
+    x[:, :, 0] = 0.0
+    got = _sample(x, u[None], **options)
+    assert np.array_equal(got[0], want), (np.flatnonzero(got[0] != want).size, got[0][:8], want[:8])
