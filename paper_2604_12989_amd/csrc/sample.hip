@@ -433,19 +433,17 @@ struct PickRow {
     int V;
     double M, c;       // largest logit, log2(e) / tau
     ArgPart floor;     // composites below it do not stay
-    double min_w;      // nor do weights below this one
+    double unit;       // units of integer weights
     double scale;      // steps of the logit for a log-weight
     // step of an element with log-weight t, in falling order
     __device__ __forceinline__ int step_of(double t) const { return min(kSteps - 1, (int)(t * scale)); }
     __device__ __forceinline__ double log_weight(float v) const { return ((double)v - M) * c; }
-    // weight of element id if it stays, else 0
-    __device__ __forceinline__ double weight(float v, int id) const
+    __device__ __forceinline__ double weight(float v) const
     {
         const double t = log_weight(v);
-        if (!(t >= kCut) || arg_part(v, id) < floor) return 0.0;
-        const double w = exp2_of(t);
-        return w >= min_w ? w : 0.0;
+        return t >= kCut ? exp2_of(t) : 0.0;
     }
+    __device__ __forceinline__ ArgPart in_units(double w) const { return (ArgPart)(w * unit + 0.5); }
     // f(value, id) for every finite element
     template <int NT, class F>
     __device__ __forceinline__ void each(F &&f) const
@@ -536,7 +534,7 @@ __device__ __forceinline__ PickRow pick_row(const float *logits, size_t row, int
     r.M = M;
     r.c = 1.4426950408889634 / (double)tau;
     r.floor = 0ull;
-    r.min_w = 0.0;
+    r.unit = 0.0;
     r.scale = kSteps / kCut;
     return r;
 }
@@ -577,27 +575,26 @@ __device__ __forceinline__ void put_token(int token, size_t row, ArgPart *part, 
     else part[row] = 1ull << 32 | (uint32_t)~token;
 }
 
-template <int NT>
 struct LocateShared {
-    double wave_d[NT / 64 < 2 ? 2 : NT / 64];
+    double wave_d[kPickThreads / 64];
     int last, token;
 };
 // The element of [start, start + n) where the running sum, `base` in front of it, exceeds `target` (the last one with a
 // weight, should rounding leave none).  c0, c1: the running sum in front of it and behind it.
-template <int NT>
-__device__ int pick_locate(const PickRow &r, int start, int n, double base, double target, LocateShared<NT> &sh, double &c0, double &c1)
+__device__ int pick_locate(const PickRow &r, int start, int n, double base, double target, LocateShared &sh, double &c0, double &c1)
 {
+    constexpr int NT = kPickThreads;
     // (a multiple of four elements a thread: as many loads of 16 bytes where the row allows)
     const int per = ((n + NT - 1) / NT + 3) / 4 * 4, from = start + (int)threadIdx.x * per, to = min(from + per, start + n);
     double mine = 0.0, total;
     int last = -1;
-    constexpr int G = NT == kPickThreads ? 6 : 1;  // groups of a thread: a segment by `pick`, a chunk by `again`
-    static_assert(4 * G * NT >= (NT == kPickThreads ? 6144 : kChunk), "the run fits");
+    constexpr int G = 6;  // groups of a thread
+    static_assert(4 * G * NT >= 6144, "a segment fits");
     float x[4 * G];
     load_run<G>(r.x, r.V, from, to, x);
 #pragma unroll
     for (int k = 0; k < 4 * G; ++k) {
-        const double w = x[k] > -INFINITY ? r.weight(x[k], from + k) : 0.0;
+        const double w = x[k] > -INFINITY ? r.weight(x[k]) : 0.0;
         if (w > 0.0) last = from + k;
         mine += w;
     }
@@ -613,7 +610,7 @@ __device__ int pick_locate(const PickRow &r, int start, int n, double base, doub
         double c = before, w = 0.0;
         int token = last;
         for (int e = from; e < to; ++e) {
-            w = r.weight(clean(r.x[e]), e);
+            w = r.weight(clean(r.x[e]));
             if (w > 0.0 && (target < c + w || e == last)) {
                 token = e;
                 break;
@@ -643,7 +640,7 @@ struct PickShared {
     };
     int32_t listed[kMaxSegs];
     ArgPart wave_u[kPickThreads / 64];
-    LocateShared<kPickThreads> locate;
+    LocateShared locate;
     int n, last, token;
 };
 
@@ -758,7 +755,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(
             const int s = sh.n;
             const double base = sh.seg[s];
             double c0, c1;
-            const int token = pick_locate<kPickThreads>(r, s * seg_len, min(seg_len, V - s * seg_len), base, target, sh.locate, c0, c1);
+            const int token = pick_locate(r, s * seg_len, min(seg_len, V - s * seg_len), base, target, sh.locate, c0, c1);
             if (slack > 0.0 && !(c0 <= (double)u * (Z - slack) && target < c1 - slack)) return put_on_list(0.0);
             return put_token(token, row, part, tokens);
         }
@@ -961,10 +958,9 @@ struct AgainShared {
             ArgPart sub[kSteps], list[kStepList], few[kStepList];
             ArgPart part[kSampleMaxV / kPart];
         } s;
-        double chunk[kMaxChunks + kAgainThreads];
+        ArgPart chunk[kMaxChunks];
     };
     ArgPart wave_u[kAgainThreads / 64];
-    LocateShared<kAgainThreads> locate;
     ArgPart found, base;
     int n, token;
 };
@@ -1019,16 +1015,15 @@ __device__ ArgPart last_in_order(ArgPart *list, int n, ArgPart front, double bou
     return r;
 }
 
-// The composite of the last element, in falling order, with less than `limit` in front of it: elements counted, or their
-// weights summed (in units of 1 / unit).  Elements below r.floor do not take part; r.floor if all stay.  However many
+// The composite of the last element, in falling order, with less than `bound` in front of it: elements counted, or (MASS) their weights
+// in units summed and `bound` a share of the sum of all.  Elements below r.floor do not take part; r.floor if all stay.  However many
 // elements lie together: equal logits are told apart by their ids.
 template <bool MASS>
-__device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, AgainShared &sh)
+__device__ ArgPart pick_threshold(const PickRow &r, double bound, AgainShared &sh)
 {
     constexpr int NT = kAgainThreads;
-    auto value = [&](double w) -> ArgPart { return MASS ? (ArgPart)(w * unit + 0.5) : 1ull; };
+    auto value = [&](double w) -> ArgPart { return MASS ? r.in_units(w) : 1ull; };
     auto bucket_of = [&](double t) { return min(kHistBuckets - 1, (int)(t * (kHistBuckets / kCut))); };
-    const double bound = MASS ? limit * unit : limit;
     int bucket = -1, shift = 64;
     ArgPart prefix = 0ull, base = 0ull;
     for (;;) {
@@ -1059,6 +1054,7 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
             mine += v[u];
         }
         ArgPart before = base + block_scan<NT>(mine, sh.wave_u, total);
+        if (MASS && bucket < 0) bound *= (double)total;
         if (bucket < 0 && (double)total < bound) return r.floor;  // all of them stay
         if (threadIdx.x == 0) sh.n = -1;
         __syncthreads();
@@ -1108,45 +1104,82 @@ __device__ ArgPart pick_threshold(const PickRow &r, double limit, double unit, A
     }
 }
 
-// A row by one workgroup: thresholds, sums of chunks, token.  For rows whose border lies among thousands of equal logits.
+__device__ __forceinline__ int step_of_min_p(const PickRow &r, float min_p)
+{
+    return min_p > 0.0f ? r.step_of(fmax(log2((double)min_p), kCut)) : kSteps;
+}
+// The last element of [start, end) that stays with at most `target` in front of it (`base` in front of `start`); PER a thread.
+template <int PER, class F>
+__device__ __forceinline__ int last_to_target(const PickRow &r, int start, int end, ArgPart base, double target, F &&stays, AgainShared &sh)
+{
+    constexpr int NT = kAgainThreads;
+    const int id0 = start + (int)threadIdx.x * PER;
+    ArgPart w[PER], mine = 0ull, total;
+    float x[PER];
+    load_run<PER / 4>(r.x, r.V, id0, min(id0 + PER, end), x);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        w[e] = x[e] > -INFINITY ? stays(x[e], id0 + e) : 0ull;
+        mine += w[e];
+    }
+    ArgPart before = base + block_scan<NT>(mine, sh.wave_u, total);
+    if (threadIdx.x == 0) sh.token = -1;
+    __syncthreads();
+    int last = -1;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (w[e] > 0ull && (double)before <= target) last = id0 + e;
+        before += w[e];
+    }
+    wave_last(&sh.token, last >= 0, last);
+    __syncthreads();
+    return sh.token;
+}
+
+// A row by one workgroup: thresholds, sums of chunks, token.  For rows whose border lies in a step with thousands of elements, and those past
+// `slots`.  The same integers are summed and compared as by the way with steps, so that a row's token does not depend on which of the
+// two it is given.  (With fp64 sums here 344 of 600 equal rows drew another token than the other 256, their uniform on a border.)
 __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float top_p, float min_p, float u, AgainShared &sh)
 {
     constexpr int NT = kAgainThreads;
-    double total;
-    r.floor = 0ull, r.min_w = 0.0;
+    ArgPart total;
+    r.floor = 0ull;
     __syncthreads();
-    if (top_k > 0) r.floor = pick_threshold<false>(r, (double)top_k, 1.0, sh);
-    if (top_p < 1.0f) {
-        double mine = 0.0;
-        r.each<NT>([&](float v, int id) { mine += r.weight(v, id); });
-        (void)block_scan<NT>(mine, sh.locate.wave_d, total);
-        r.floor = pick_threshold<true>(r, (double)top_p * total, unit_of(total), sh);
-    }
-    r.min_w = (double)min_p;
+    if (top_k > 0) r.floor = pick_threshold<false>(r, (double)top_k, sh);
+    if (top_p < 1.0f) r.floor = pick_threshold<true>(r, (double)top_p, sh);
+    // (from the step where min-p ends on weights are looked at, behind it none stays; the last one has no end)
+    const int min_step = step_of_min_p(r, min_p);
+    const double from_step = min_step < kSteps ? min_step : 1e30, past_step = min_step < kSteps - 1 ? min_step + 1 : 1e30;
+    auto stays = [&](float v, int id) -> ArgPart {
+        const double t = r.log_weight(v), step = t * r.scale;
+        if (!(t >= kCut) || step >= past_step || arg_part(v, id) < r.floor) return 0ull;
+        const double weight = exp2_of(t);
+        return step >= from_step && weight < (double)min_p ? 0ull : r.in_units(weight);
+    };
     const int chunks = (r.V + kChunk - 1) / kChunk, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int k = wave; k < chunks; k += NT / 64) {
         const int start = k * kChunk, from = start + lane * (kChunk / 64);
-        double sum = 0.0;
+        ArgPart sum = 0ull;
         float x[kChunk / 64];
         load_run<kChunk / 256>(r.x, r.V, from, min(from + kChunk / 64, r.V), x);
 #pragma unroll
-        for (int e = 0; e < kChunk / 64; ++e) sum += x[e] > -INFINITY ? r.weight(x[e], from + e) : 0.0;
-        sum = wave_sum_f64_lane63(sum);
+        for (int e = 0; e < kChunk / 64; ++e) sum += x[e] > -INFINITY ? stays(x[e], from + e) : 0ull;
+        sum = wave_scan64(sum);
         if (lane == 63) sh.chunk[k] = sum;
     }
     __syncthreads();
     const int per = (chunks + NT - 1) / NT, from = (int)threadIdx.x * per, to = min(from + per, chunks);
-    double mine = 0.0;
+    ArgPart mine = 0ull;
     for (int k = from; k < to; ++k) mine += sh.chunk[k];
-    double before = block_scan<NT>(mine, sh.locate.wave_d, total);
-    const double target = (double)u * total;
+    ArgPart before = block_scan<NT>(mine, sh.wave_u, total);
+    const double target = (double)u * (double)total;
     if (threadIdx.x == 0) sh.n = -1;
     __syncthreads();
     // the last chunk with a weight that has at most the target in front of it
     int last = -1;
     for (int k = from; k < to; ++k) {
-        const double w = sh.chunk[k];
-        if (w > 0.0 && before <= target) last = k;
+        const ArgPart w = sh.chunk[k];
+        if (w > 0ull && (double)before <= target) last = k;
         sh.chunk[k] = before;  // from now on: the sum in front of it
         before += w;
     }
@@ -1154,10 +1187,7 @@ __device__ __attribute__((noinline)) int pick_alone(PickRow r, int top_k, float 
     __syncthreads();
     const int k = sh.n;
     if (k < 0) return -1;
-    const double base = sh.chunk[k];
-    __syncthreads();
-    double c0, c1;
-    return pick_locate<NT>(r, k * kChunk, min(kChunk, r.V - k * kChunk), base, target, sh.locate, c0, c1);
+    return last_to_target<4>(r, k * kChunk, min((k + 1) * kChunk, r.V), sh.chunk[k], target, stays, sh);
 }
 
 // Weight and count of the thread's step over a row, from its parts' sums (threads past the steps: nothing).
@@ -1179,14 +1209,10 @@ __device__ __forceinline__ void step_totals(const StepSum *steps, int parts, Arg
         }
     }
 }
-__device__ __forceinline__ int step_of_min_p(const PickRow &r, float min_p)
-{
-    return min_p > 0.0f ? r.step_of(fmax(log2((double)min_p), kCut)) : kSteps;
-}
 
 // The border from the steps' sums, then the token.  `few`: the elements of step `ready`, gathered by others.  False: too many elements
 // in the border's step.
-__device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts, double unit, int top_k, float top_p, float min_p,
+__device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts, int top_k, float top_p, float min_p,
                               float u, int ready, int listed, const ArgPart *few, AgainShared &sh, int &token)
 {
     constexpr int NT = kAgainThreads;
@@ -1232,7 +1258,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         __syncthreads();
         return true;
     };
-    auto weight_of = [&](ArgPart c) { return (ArgPart)(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32)))) * unit + 0.5); };
+    auto weight_of = [&](ArgPart c) { return r.in_units(exp2_of(r.log_weight(key_float((uint32_t)(c >> 32))))); };
     // Of the gathered step the composite of the last element with less than `limit` in front of it: once more by steps, 256 of
     // the step, and the elements of one of those against one another.
     auto sub_step = [&](ArgPart c) {
@@ -1295,7 +1321,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
                 border = at;
                 floor = 0ull;
                 if (!gather(border)) return false;
-                }
+            }
             const ArgPart found = last_in_step(true, s.mass[border], limit);
             if (found != ~0ull && found > floor) floor = found;
         }
@@ -1311,7 +1337,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         const int step = r.step_of(t);
         if (step > border || (step == border && arg_part(v, id) < floor)) return 0ull;
         const double weight = exp2_of(t);
-        return step == border && weight < (double)min_p ? 0ull : (ArgPart)(weight * unit + 0.5);
+        return step == min_step && weight < (double)min_p ? 0ull : r.in_units(weight);
     };
     // ---- weights of the parts: steps in front of the border, and the border's elements ----
     for (int p = tid; p < parts; p += NT) s.part[p] = steps[(size_t)p * (kSteps + 1) + border].mass;
@@ -1325,7 +1351,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
         }
     __syncthreads();
     const int per = (parts + NT - 1) / NT, from = tid * per, to = min(from + per, parts);
-    ArgPart mine = 0ull, S, total;
+    ArgPart mine = 0ull, S;
     for (int p = from; p < to; ++p) mine += s.part[p];
     ArgPart before = block_scan<NT>(mine, sh.wave_u, S);
     const double target = (double)u * (double)S;
@@ -1343,30 +1369,7 @@ __device__ bool pick_by_steps(const PickRow &r, const StepSum *steps, int parts,
     __syncthreads();
     const int p = sh.n;
     if (p < 0) return false;
-    const ArgPart base = s.part[p];
-    constexpr int kEach = kPart / NT;
-    const int id0 = p * kPart + tid * kEach;
-    ArgPart w[kEach];
-    mine = 0ull;
-    float x[kEach];
-    load_run<kEach / 4>(r.x, r.V, id0, min(id0 + kEach, r.V), x);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        w[e] = x[e] > -INFINITY ? stays(x[e], id0 + e) : 0ull;
-        mine += w[e];
-    }
-    before = base + block_scan<NT>(mine, sh.wave_u, total);
-    if (tid == 0) sh.token = -1;
-    __syncthreads();
-    last = -1;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        if (w[e] > 0ull && (double)before <= target) last = id0 + e;
-        before += w[e];
-    }
-    wave_last(&sh.token, last >= 0, last);
-    __syncthreads();
-    token = sh.token;
+    token = last_to_target<kPart / NT>(r, p * kPart, min((p + 1) * kPart, r.V), s.part[p], target, stays, sh);
     return true;
 }
 
@@ -1385,9 +1388,8 @@ __global__ __launch_bounds__(kStepThreads) void sample_steps_kernel(
         const HardRow row = hard[h];
         const int seq = row.row / T;
         const bool by_count = opt.top_k[seq] > 0;
-        const double unit = row.unit;
         PickRow r = pick_row(logits, (size_t)row.row, V, row.best, opt.tau[seq]);
-        r.scale = row.scale;
+        r.unit = row.unit, r.scale = row.scale;
         const int start = p * kPart;
         const Run run(r.x + start, min(kPart, V - start));
         constexpr int G = kPart / (4 * NT);
@@ -1404,7 +1406,7 @@ __global__ __launch_bounds__(kStepThreads) void sample_steps_kernel(
             const double t = v > -INFINITY ? r.log_weight(v) : 2.0 * kCut;
             if (!(t >= kCut)) return;
             const int step = r.step_of(t);
-            atomicAdd(&s_mass[step], (ArgPart)(exp2_of(t) * unit + 0.5));
+            atomicAdd(&s_mass[step], r.in_units(exp2_of(t)));
             if (by_count) atomicAdd(&s_count[step], 1u);
         };
 #pragma unroll
@@ -1481,11 +1483,11 @@ __global__ __launch_bounds__(kAgainThreads) void sample_again_kernel(
         const int seq = row.row / T, top_k = opt.top_k[seq];
         const float top_p = opt.top_p[seq], min_p = opt.min_p[seq], u = clean_uniform(uniforms[row.row]);
         PickRow r = pick_row(logits, (size_t)row.row, V, row.best, opt.tau[seq]);
-        r.scale = row.scale;
+        r.unit = row.unit, r.scale = row.scale;
         int token = -1;
         __syncthreads();  // (the shared memory of the row before)
         if (h >= slots ||
-            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, row.unit, top_k, top_p, min_p, u, row.border,
+            !pick_by_steps(r, steps + (size_t)h * parts * (kSteps + 1), parts, top_k, top_p, min_p, u, row.border,
                            row.listed, few + (size_t)h * kStepList, sh, token))
             token = pick_alone(r, top_k, top_p, min_p, u, sh);
         put_token(token, (size_t)row.row, part, tokens);

@@ -1,4 +1,5 @@
-"""Rows that are read again, with uniforms next to a border: the sums that decide hold to what the definition says."""
+"""Rows that are read again, with uniforms next to a border: the sums that decide hold to what the definition says, and a row's
+token does not depend on which rows share the call."""
 import numpy as np
 import pytest
 import torch
@@ -37,3 +38,22 @@ def test_a_likely_token_and_equal_others(options, kept):
     x[:, :, 0] = 0.0
     got = _sample(x, u[None], **options)
     assert np.array_equal(got[0], want), (np.flatnonzero(got[0] != want).size, got[0][:8], want[:8])
+
+
+@pytest.mark.parametrize("options", [dict(min_p=0.001), dict(top_k=1500), dict(top_k=700), dict(top_k=1500, min_p=0.001),
+                                     dict(top_k=700, top_p=0.9999999)])
+@pytest.mark.parametrize("half", [1501, 2750])
+def test_rows_in_two_equal_halves(half, options):
+    """u = 1/2 of a row whose second half repeats the first: the running sum in front of the second half is exactly half of
+    all, so that the token is the first of the second half that stays.  600 times the same row, more than have room together;
+    twice."""
+    for seed in range(6):
+        x = (0.5 * np.random.default_rng(seed).standard_normal(half)).astype(np.float32)
+        order = np.lexsort((np.arange(2 * half), -np.concatenate([x, x])))
+        stays = order[:options.get("top_k", 2 * half)]
+        want = stays[stays >= half].min()
+        rows = np.broadcast_to(np.concatenate([x, x]), (2, 300, 2 * half))
+        u = np.full((2, 300), 0.5)
+        first = _sample(rows, u, **options)
+        assert (first == want).all(), (seed, want, np.unique(first, return_counts=True))
+        assert np.array_equal(_sample(rows, u, **options), first)
