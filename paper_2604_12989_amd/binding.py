@@ -373,6 +373,13 @@ def accept_filtered(target_logits, tokens, parent, depth, n_nodes, B, uniforms, 
         n_accepted = torch.empty_like(n_nodes)
         out = dict(path=n_nodes.new_empty((batch, B + 1)), n_accepted=n_accepted, bonus_token=torch.empty_like(n_accepted),
                    posterior=torch.empty_like(tokens) if want_posterior else None)
+    else:
+        for name, count in (("path", batch * (B + 1)), ("n_accepted", batch), ("bonus_token", batch), ("posterior", batch * T)):
+            t = out.get(name)
+            if t is None and name == "posterior":
+                continue
+            if _dev(t, torch.int32, name).numel() != count or t.get_device() != target_logits.get_device():
+                raise DDTreeError(f"{name}: expected {count} entries on the device of target_logits")
     arrays, ptrs = _options(batch, temperature, top_k, top_p, min_p)
     p, n = _ws(ws)
     args = (_ptr(target_logits), batch, T, V, _ptr(tokens), _ptr(parent), _ptr(depth), _ptr(n_nodes), *ptrs, _ptr(uniforms),
