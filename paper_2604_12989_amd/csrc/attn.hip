@@ -1142,14 +1142,14 @@ static int verify_attn_impl(const void *q, const void *k_cache, const void *v_ca
                            static_cast<const uint16_t *>(v_tree), ancestor_mask, args, T, Hq, Hkv, softmax_scale * kLog2e,
                            static_cast<uint16_t *>(out), part, lse, *c4);
             } else {
-            auto *kernel = p.wide ? attn_mfma_kernel<true> : attn_mfma_kernel<false>;
-            if (!allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kAttnLdsBytes, lds_allowed[p.wide ? 1 : 0]))
-                return DDTREE_ERR_HIP;
-            DDT_LAUNCH(DDTREE_KERNEL_ATTN, st, kernel, dim3((unsigned)args.grid), dim3(kAttnThreads),
-                       kAttnLdsBytes, st, static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_cache),
-                       static_cast<const uint16_t *>(v_cache), static_cast<const uint16_t *>(k_tree),
-                       static_cast<const uint16_t *>(v_tree), ancestor_mask, args, T, Hq, Hkv,
-                       softmax_scale * kLog2e, static_cast<uint16_t *>(out), part, lse);
+                auto *kernel = p.wide ? attn_mfma_kernel<true> : attn_mfma_kernel<false>;
+                if (!allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kAttnLdsBytes, lds_allowed[p.wide ? 1 : 0]))
+                    return DDTREE_ERR_HIP;
+                DDT_LAUNCH(DDTREE_KERNEL_ATTN, st, kernel, dim3((unsigned)args.grid), dim3(kAttnThreads),
+                           kAttnLdsBytes, st, static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_cache),
+                           static_cast<const uint16_t *>(v_cache), static_cast<const uint16_t *>(k_tree),
+                           static_cast<const uint16_t *>(v_tree), ancestor_mask, args, T, Hq, Hkv,
+                           softmax_scale * kLog2e, static_cast<uint16_t *>(out), part, lse);
             }
         }
         if (most > 1) {

@@ -1570,9 +1570,13 @@ static int sample_rows(const float *logits, int batch, int T, int V, const int32
                p.hot, p.hot_cap, n_nodes, stat, hot, n_hard, opt);
     DDT_LAUNCH(DDTREE_KERNEL_SAMPLE_PICK, st, sample_pick_kernel, dim3(T, batch), dim3(kPickThreads), 0, st, logits, T, V, p.seg_len, p.segs,
                p.hot_cap, n_nodes, uniforms, stat, hot, *part, tokens, n_hard, hard, opt);
-    // (a row goes on the list by what its logits are: these look whether there are any)
-    // Rows of a small top-k or without filters are hardly ever on it, and are then read as often as it takes: no launch for
-    // their steps (257 rows of 151936 by top-k 50: 51 -> 48 us).
+    // (A row goes on the list by what its logits are: these look whether there are any.)
+    // The launches for their steps are made where some sequence's rows are often on it: top-p or min-p alone, or a top-k above 700.  Other rows
+    // that get there are read as often as it takes, by a workgroup each.  These are rows of a top-k beyond what their lists hold above the
+    // largest of the bounds (elements of rows at random: some 200 for V = 2000, 500 to 900 with 75 segments of 2048, 950 to 1250 with 25 of 6144), and
+    // rows with many of the likely ids in one segment.  Without the launches 257 rows of 151936 by top-k 50 take 48 us instead
+    // of 51; but where 16 rows by top-k 701 take 28 us from the list on, by top-k 700 it is 185, and 257 rows by top-k 50 whose first
+    // 6144 logits are higher by 2 take 190.
     bool shared = false;
     for (int s = 0; s < batch; ++s)
         shared = shared || (opt.tau[s] > 0.0f && (opt.top_k[s] > 700 || (opt.top_k[s] == 0 && (opt.top_p[s] < 1.0f || opt.min_p[s] > 0.0f))));
