@@ -243,8 +243,12 @@ int ddtree_accept_sampled(const float *target_logits, int batch, int T, int V,
  *     min_p    w_v >= min_p                                                         (0: off)
  * so the likeliest token always stays.  The token is the first that stays, by ascending id, whose running sum of w (its own
  * included) exceeds u times the sum of all that stay.  temperature = 0: the likeliest token, of equal ones the lowest id.
- * Logits of -inf are never selected (nor NaN); a row of nothing else gives -1.  Weights and sums are taken in fp64: a
- * token differs from this definition's only where u lies within about 1e-12 of a border.
+ * Logits of -inf are never selected (nor NaN, of either kind); +inf counts as the largest finite number; a row of nothing else
+ * than -inf and NaN gives -1.  Weights are taken in fp64, sums in fp64 or in 64-bit integers of them; three comparisons are decided by their
+ * rounding where both sides lie close together, within about 1e-12 of the row's sum (6e-11 at the largest V, with equal weights, which are
+ * all rounded alike) or 1e-15 of a weight: u times the sum with a running sum (the token is then one of two neighbours), top_p times the
+ * sum with what is in front of an element, and a weight with min_p (the element then stays or does not, and other u may select
+ * another token).  The same call gives the same tokens whenever it is made, and equal rows of a sequence with equal uniforms the same one.
  *   logits      [device] fp32 [batch, T, V], V <= 2^22
  *   temperature, top_k, top_p, min_p   [host] fp32 / int32 / fp32 / fp32 [batch]; temperature >= 0 and at most 1e30, top_k >= 0,
  *               0 < top_p <= 1, 0 <= min_p <= 1 (DDTREE_ERR_ARG otherwise); the last three nullable (off)

@@ -31,9 +31,10 @@ void attn_wave_kernel(const AttnWaveArgs args)
     attn_wave_rows<D, RB, WIDE>(args, item);
 }
 
-// The same over a 4-bit cache.  Bound by vector issue, not by the cache's bytes: a step of eight sub-tiles takes 1.18 us as over bf16 rows
+// The same over a 4-bit cache.  Bound by issue and the waits between, with two waves a SIMD, not by the cache's bytes (17 nodes over 32768 keys:
+// vector instructions on 45 % of a SIMD's time, matrix cores 27 %, a wave at s_waitcnt 34 %): a step of eight sub-tiles takes 1.18 us as over bf16 rows
 // from the L2 (64 conversions, 16 exponentials and some 150 other instructions a wave), 1.34 with all compute units at work.  8 sequences of
-// 8192 keys, a token each, 32 query and 8 KV heads: 20 us (bf16 rows, which come from HBM, 56); 32 sequences, 64 heads: 55.5 (200).
+// 8192 keys, a token each, 32 query and 8 KV heads: 20.5 us with the merge (bf16 rows, which come from HBM, 49); 32 sequences, 64 heads: 55 (192).
 template <int D, int RB, bool WIDE>
 __global__ __launch_bounds__((WaveShape<D, RB>::threads))
 __attribute__((amdgpu_waves_per_eu(WaveShape<D, RB>::waves / 4, WaveShape<D, RB>::waves / 4)))

@@ -20,8 +20,12 @@
 //          front of each of 256 steps of the logit; they add these up and gather the elements of the one step where the
 //          border lies; then one puts those in order and draws the token.  (In one launch, the last workgroup of a row going
 //          on by itself, the fences between the XCDs' caches took 20 times as long as the work.)
-// Measured, 257 rows of 151936, top-k 50: scan 28.8 us (5.4 TB/s), pick 11, the empty list 2; 256 flat rows, top-p 0.95: scan 62
-// (some 25 fp64 operations an element), pick 23, steps 71, gather 82, again 23; one flat row 5.5, 15, 6, 8, 18.
+// Measured (begin to end of each launch), 257 rows of 151936, top-k 50: scan 28 to 30 us (5.2 to 5.5 TB/s), pick 11, the empty list 4.  256 flat
+// rows, N(0, 1/4), top-p 0.95: scan 65 (some 25 fp64 operations an element), pick 25, steps 73, gather 85, again 25 (of 257, one row without a
+// place, 309); one flat row: 6, 18, 6, 8, 20.  Rows whose border lies in a step with more than kStepList
+// elements are left to one workgroup each: equal logits, but also flat rows by min-p or a large top-k, where the steps are as
+// wide as the 40 powers of two that weights span make them (again: 16 rows N(0, 4) at temperature 2 by min-p 0.02: 95 us; 16 rows
+// N(0, 1/4) by top-k 20000: 242; 16 rows of equal logits by top-p: 1.7 ms).
 // Sums that are taken with atomics are integers (weights in units of 2^-52 of the largest, or as fine as 63 bits allow):
 // their order does not matter.
 #include <algorithm>
