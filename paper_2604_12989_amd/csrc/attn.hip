@@ -101,7 +101,7 @@ static_assert(WaveShape<kHD, 1>::threads == kAttnThreads && WaveShape<kHD, 1>::l
 // Q4: the cache holds 4-bit codes.  A cache tile is then 4 KB of codes and 256 B of scales for K and as much for V: thread t
 // loads one block of 32 elements (K: the first half of the threads, V: the second) one step ahead of its use, and
 // writes it to the ring as bf16, which from there on is what the loads of a bf16 cache leave.  (257 nodes x 8192 keys: 47.4 us, 44.7 over
-// bf16 rows on the same box; decoded once for the eight waves, 16 conversions and four LDS writes a thread and tile of 32 matrix instructions.)
+// bf16 rows, measured together; decoded once for the eight waves, 16 conversions and four LDS writes a thread and tile of 32 matrix instructions.)
 template <bool WIDE, bool Q4>
 __device__ __forceinline__ void attn_mfma_body(
                       const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_cache,

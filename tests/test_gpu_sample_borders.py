@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests import gpu_util as gu
+from tests import sample_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,18 @@ def test_rows_in_two_equal_halves(half, options):
         first = _sample(rows, u, **options)
         assert (first == want).all(), (seed, want, np.unique(first, return_counts=True))
         assert np.array_equal(_sample(rows, u, **options), first)
+
+
+@pytest.mark.parametrize("V,T,scale,higher,options", [
+    (2000, 64, 2.0, 0, dict(top_k=300)), (12000, 24, 2.0, 0, dict(top_k=500)), (151936, 4, 2.0, 0, dict(top_k=700)),
+    (151936, 24, 2.0, 6144, dict(top_k=50)), (151936, 24, 2.0, 6144, dict(top_k=50, top_p=0.95)),
+    (151936, 6, 2.0, 0, dict(temperature=2.0, min_p=0.02)), (151936, 4, 0.5, 0, dict(top_k=20000, min_p=0.3))])
+def test_rows_that_one_workgroup_reads_alone(V, T, scale, higher, options):
+    """A top-k that the lists do not hold in a call without the launches for steps, likely ids side by side, a border in a step with
+    thousands of elements."""
+    rng = np.random.default_rng(V + T)
+    x = (scale * rng.standard_normal((1, T, V))).astype(np.float32)
+    x[:, :, :higher] += 2.0
+    u = rng.random((1, T)).astype(np.float32)
+    want = sample_ref.tokens(x, u, **{"tau": 1.0, **{"tau" if k == "temperature" else k: v for k, v in options.items()}})
+    assert np.array_equal(_sample(x, u, **options), want)
